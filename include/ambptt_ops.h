@@ -1,0 +1,146 @@
+/*
+ * ambptt — operators of a residual block over a long sequence, on one AMD
+ * Instinct MI355X (gfx950): attention whose state decays, dropout from a
+ * counter-based generator, and the root-mean-square norm behind a residual's
+ * addition.  They are what a block puts around its products: the attention is
+ * a recurrence whose state is what a checkpoint holds, dropout's mask is
+ * generated again wherever a step is evaluated again, and the norm keeps a
+ * deep stack's activations in range.
+ *
+ * Conventions, beside those of ambptt.h
+ *   - No context: every call enqueues its kernels on `stream` (hipStream_t,
+ *     NULL = the null stream) of the current device and returns.  Nothing is
+ *     allocated, nothing waits; calls may be captured in a HIP graph.
+ *   - The caller owns all device memory, the workspace among it (its size from
+ *     the *_workspace call, 256-byte aligned).  Calls in flight at the same
+ *     time need workspaces of their own.
+ *   - Two runs on the same inputs give the same bits.
+ *   - EINVAL / EUNSUPPORTED: nothing was enqueued.  EHIP: a launch failed.
+ *   - Operands are fp32 or bf16 (AMBPTT_F32, AMBPTT_BF16); states, decays,
+ *     norm weights and their gradients, scales, sums and statistics are fp32.
+ */
+#ifndef AMBPTT_OPS_H
+#define AMBPTT_OPS_H
+
+#include "ambptt.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---- attention with a decaying state --------------------------------------
+ *
+ * For batch row b and key/value head h, with lambda = exp(log_decay[h]) and a
+ * state S [dk][dv]:
+ *   S_i = lambda S_{i-1} + k_i v_i^T,   o_i = scale S_i^T q_i,
+ * for the row's first lengths[b] tokens (all without lengths).  Query head
+ * h * group + g reads the state of key/value head h.  Outputs of the tokens
+ * past a row's length are zero, and nothing in their inputs is used.
+ *
+ * Gradients, with D_n the gradient of the last state:
+ *   A_i = D_i + scale sum_g q_i do_i^T,  dk_i = A_i v_i,  dv_i = A_i^T k_i,
+ *   D_{i-1} = lambda A_i,  dq_i = scale S_i do_i.
+ * The decay is a constant of the head: it has no gradient here. */
+typedef struct {
+  int32_t dtype;      /* AMBPTT_F32 | AMBPTT_BF16: q, k, v, o and their gradients */
+  int32_t batch;      /* >= 1 */
+  int32_t heads;      /* key/value heads, >= 1 */
+  int32_t group;      /* query heads per key/value head, >= 1 */
+  int32_t dk, dv;     /* multiples of 16 from 16 to 128 */
+  int64_t steps;      /* tokens per row, 0 .. 2^31 - 1 */
+  float scale;        /* of the queries' products, usually 1 / sqrt(dk) */
+} ambptt_attention;
+
+/* A [batch][steps][heads][size] operand anywhere in memory: element (b, t, h, i)
+ * is at p[b * batch + t * step + h * head + i], strides in elements, >= 0
+ * (zero strides broadcast an input; an output's elements must not overlap). */
+typedef struct {
+  void* p;
+  int64_t batch, step, head;
+} ambptt_view;
+
+/* Bytes of workspace that the forward (backward 0) or backward call needs; may
+ * be 0.  Pure host. */
+ambptt_status ambptt_decay_attention_workspace(const ambptt_attention* a, int32_t backward, size_t* bytes);
+
+/* o and the last state.  s0, sn: fp32 [batch][heads][dk][dv]; s0 NULL = zeros;
+ * sn may be NULL, and may be s0 (the state of a generator, advanced in place).
+ * lengths int32 [batch] on the device, or NULL; values outside 0 .. steps count
+ * as the nearer of the two.  One token (steps = 1) reads and writes the state
+ * once and multiplies nothing else. */
+ambptt_status ambptt_decay_attention(const ambptt_attention* a, const ambptt_view* q, const ambptt_view* k,
+                                     const ambptt_view* v, const float* log_decay, const float* s0,
+                                     const int32_t* lengths, const ambptt_view* o, float* sn, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/* Gradients of q, k, v and, where ds0 is given, of s0.  dsn: the gradient of
+ * the last state, NULL = zeros.  The states are formed again from s0, k and v;
+ * nothing is kept from the forward call. */
+ambptt_status ambptt_decay_attention_backward(const ambptt_attention* a, const ambptt_view* q, const ambptt_view* k,
+                                              const ambptt_view* v, const float* log_decay, const float* s0,
+                                              const int32_t* lengths, const ambptt_view* d_o, const float* dsn,
+                                              const ambptt_view* dq, const ambptt_view* dk, const ambptt_view* dv,
+                                              float* ds0, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- dropout ----------------------------------------------------------------
+ *
+ * The mask is a function of (seed, offset, row, column) and is stored nowhere:
+ * the call that forms a gradient, or a step again, gives the same numbers and
+ * finds the same mask.  Column c of row r takes half c % 2 (0: the low one) of
+ * word (c % 8) / 2 of Philox-4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel
+ * random numbers: as easy as 1, 2, 3", 2011) at the counter
+ * offset + r ceil(cols / 8) + c / 8 (64 bits, the upper 64 of the 128 are zero)
+ * under the key seed.  The element is kept where these 16 bits are not below
+ * t = round(65536 p), and then multiplied by 65536 / (65536 - t), so that the
+ * expectation is exact for the probability t / 65536 that is used.  A dropped
+ * element gives zero whatever it holds.  A call uses rows * ceil(cols / 8)
+ * counters.  p = 0 keeps all, p = 1 nothing. */
+typedef struct {
+  double p;            /* 0 .. 1 */
+  uint64_t seed, offset;
+} ambptt_drop;
+
+/* y = residual + dropout(x); residual NULL = none (then the call on a gradient
+ * gives dropout's gradient).  Rows of `cols` elements with row strides ld* in
+ * elements; y may be x or residual. */
+ambptt_status ambptt_dropout(int32_t dtype, int64_t rows, int64_t cols, const ambptt_drop* drop, const void* x,
+                             int64_t ldx, const void* residual, int64_t ldr, void* y, int64_t ldy, void* stream);
+
+/* ---- root-mean-square norm with the residual's addition -----------------------
+ *
+ *   h = residual + dropout(x),   y = w h / sqrt(mean(h^2) + eps)
+ * row by row, h and y in fp32 until they are stored. */
+enum { AMBPTT_F8 = 2 };  /* y in 8 bits: OCP e4m3, y ~= scale * stored, scale = max|y| / 448 */
+
+typedef struct {
+  int32_t dtype;        /* AMBPTT_F32 | AMBPTT_BF16: x, residual, h and the gradients */
+  int32_t out;          /* y: dtype, or AMBPTT_F8 */
+  int64_t rows, cols;   /* rows >= 0, 1 <= cols < 2^31 */
+  int32_t scale_block;  /* F8: columns per scale, 0 (one per row) or 128 */
+  float eps;
+} ambptt_norm;
+
+/* residual and drop may be NULL (none); h may be NULL (not stored), and may be
+ * x or residual.  w fp32 [cols].  scale: fp32 [rows][ceil(cols / scale_block)]
+ * (one per row with scale_block 0), for F8; a block of zeros gets the scale 1. */
+ambptt_status ambptt_add_norm(const ambptt_norm* n, const ambptt_drop* drop, const void* x, int64_t ldx,
+                              const void* residual, int64_t ldr, const float* w, void* h, int64_t ldh, void* y,
+                              int64_t ldy, float* scale, void* stream);
+
+/* Gradients, from dy (of y), dh (of h; NULL = zeros), the stored h and w:
+ *   dr = dh + r (w dy - h r^2 mean(w dy h)),  r = 1 / sqrt(mean(h^2) + eps),
+ *   dx = dr through dropout,  dw = sum over the rows of dy h r.
+ * dr is the residual's gradient (and x's, without dropout).  dx may be NULL
+ * without dropout, dw may be NULL (the weight is a constant); dr may be dy or
+ * dh.  n->out is not looked at. */
+ambptt_status ambptt_add_norm_backward_workspace(const ambptt_norm* n, size_t* bytes);
+ambptt_status ambptt_add_norm_backward(const ambptt_norm* n, const ambptt_drop* drop, const void* dy, int64_t lddy,
+                                       const void* dh, int64_t lddh, const void* h, int64_t ldh, const float* w,
+                                       void* dr, int64_t lddr, void* dx, int64_t lddx, float* dw, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* AMBPTT_OPS_H */

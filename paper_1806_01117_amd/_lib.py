@@ -10,6 +10,7 @@ LIB_PATH = os.path.join(_HERE, "libambptt.so")
 OK, EINVAL, ENOMEM, EHIP, EUNSUPPORTED, EINTERNAL = 0, -1, -2, -3, -4, -5
 CELL = {"rnn": 1, "lstm": 2, "resmlp": 3, "mlp": 4}
 DTYPE = {"f32": 0, "bf16": 1}
+F8 = 2  # of add_norm's y
 LOSS = {"half_sq_last": 0, "mean_sq_all": 1, "mean_last": 2}
 
 EXPORTS = ["ambptt_version", "ambptt_revolve_advances", "ambptt_schedule_evals", "ambptt_schedule_text",
@@ -17,7 +18,9 @@ EXPORTS = ["ambptt_version", "ambptt_revolve_advances", "ambptt_schedule_evals",
            "ambptt_interval_from_timings", "ambptt_set_step_costs", "ambptt_set_widths",
            "ambptt_resident_program", "ambptt_query", "ambptt_last_error",
            "ambptt_create", "ambptt_bind", "ambptt_workspace_bytes", "ambptt_set_int", "ambptt_set_file_tier", "ambptt_calibrate", "ambptt_run", "ambptt_run_noalloc",
-           "ambptt_last_schedule_text", "ambptt_destroy"]
+           "ambptt_last_schedule_text", "ambptt_destroy",
+           "ambptt_decay_attention_workspace", "ambptt_decay_attention", "ambptt_decay_attention_backward",
+           "ambptt_dropout", "ambptt_add_norm", "ambptt_add_norm_backward_workspace", "ambptt_add_norm_backward"]
 
 
 class Problem(C.Structure):
@@ -25,6 +28,24 @@ class Problem(C.Structure):
                 ("batch", C.c_int32), ("input", C.c_int32), ("hidden", C.c_int32),
                 ("n_steps", C.c_int64), ("fast_slots", C.c_int32), ("interval_min", C.c_int32),
                 ("slow_slots", C.c_int64)]
+
+
+class Attention(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("batch", C.c_int32), ("heads", C.c_int32), ("group", C.c_int32),
+                ("dk", C.c_int32), ("dv", C.c_int32), ("steps", C.c_int64), ("scale", C.c_float)]
+
+
+class View(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("batch", C.c_int64), ("step", C.c_int64), ("head", C.c_int64)]
+
+
+class Drop(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("offset", C.c_uint64)]
+
+
+class Norm(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("out", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("scale_block", C.c_int32), ("eps", C.c_float)]
 
 
 class Stats(C.Structure):
@@ -119,6 +140,17 @@ def load():
     L.ambptt_run_noalloc.restype = C.c_int
     L.ambptt_destroy.argtypes = [vp]
     L.ambptt_destroy.restype = None
+    att, view, nrm, drop = C.POINTER(Attention), C.POINTER(View), C.POINTER(Norm), C.POINTER(Drop)
+    L.ambptt_decay_attention_workspace.argtypes = [att, i32, C.POINTER(sz)]
+    L.ambptt_decay_attention.argtypes = [att, view, view, view, vp, vp, vp, view, vp, vp, sz, vp]
+    L.ambptt_decay_attention_backward.argtypes = [att, view, view, view, vp, vp, vp, view, vp, view, view, view, vp, vp,
+                                                  sz, vp]
+    L.ambptt_dropout.argtypes = [i32, i64, i64, drop, vp, i64, vp, i64, vp, i64, vp]
+    L.ambptt_add_norm.argtypes = [nrm, drop, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp]
+    L.ambptt_add_norm_backward_workspace.argtypes = [nrm, C.POINTER(sz)]
+    L.ambptt_add_norm_backward.argtypes = [nrm, drop, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, sz, vp]
+    for f in EXPORTS[-7:]:
+        getattr(L, f).restype = C.c_int
     _lib = L
     return L
 

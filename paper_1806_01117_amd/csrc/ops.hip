@@ -1,0 +1,228 @@
+// C entries of the operators: checks of the arguments, and the launches.
+#include "ops.hpp"
+
+#include <cmath>
+#include <exception>
+
+using namespace ambptt;
+
+namespace {
+
+#define REFUSE(cond, status, msg) \
+  do {                            \
+    if (cond) return fail_with(status, msg); \
+  } while (0)
+
+ambptt_status done(hipError_t e) {
+  return e == hipSuccess ? AMBPTT_OK : fail_with(AMBPTT_EHIP, hipGetErrorString(e));
+}
+
+// the bytes of an element, 0 for an unknown dtype
+int size_of(int32_t dtype) { return dtype == AMBPTT_F32 ? 4 : dtype == AMBPTT_BF16 ? 2 : 0; }
+
+bool misaligned(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
+
+ambptt_status check_attention(const ambptt_attention* a) {
+  REFUSE(!a, AMBPTT_EINVAL, "attention is NULL");
+  REFUSE(!size_of(a->dtype), AMBPTT_EINVAL, "unknown dtype");
+  REFUSE(a->batch < 1 || a->heads < 1 || a->group < 1, AMBPTT_EINVAL, "batch, heads and group must be positive");
+  REFUSE(a->dk < 1 || a->dv < 1, AMBPTT_EINVAL, "head sizes must be positive");
+  REFUSE(a->steps < 0, AMBPTT_EINVAL, "steps must be >= 0");
+  REFUSE(!std::isfinite(a->scale), AMBPTT_EINVAL, "scale must be finite");
+  REFUSE(a->dk % 16 || a->dv % 16 || a->dk > 128 || a->dv > 128, AMBPTT_EUNSUPPORTED,
+         "head sizes must be multiples of 16 from 16 to 128");
+  REFUSE(a->steps > INT32_MAX, AMBPTT_EUNSUPPORTED, "steps must be below 2^31");
+  REFUSE((int64_t)a->batch * a->heads > (int64_t(1) << 24) || (int64_t)a->heads * a->group > (int64_t(1) << 24),
+         AMBPTT_EUNSUPPORTED, "more than 2^24 states or query heads");
+  return AMBPTT_OK;
+}
+
+// v: NULL, or a view whose elements are not all there; out: what is written may not overlap
+ambptt_status check_view(const ambptt_attention* a, const ambptt_view* v, int heads, int size, bool out) {
+  REFUSE(!v || (!v->p && a->steps > 0), AMBPTT_EINVAL, "an operand is NULL");
+  REFUSE(misaligned(v->p, size_of(a->dtype)), AMBPTT_EINVAL, "an operand is not aligned to its elements");
+  REFUSE(v->batch < 0 || v->step < 0 || v->head < 0, AMBPTT_EINVAL, "strides must be >= 0");
+  if (out) {
+    REFUSE((a->batch > 1 && v->batch < size) || (a->steps > 1 && v->step < size) || (heads > 1 && v->head < size),
+           AMBPTT_EINVAL, "an output's elements overlap");
+  }
+  return AMBPTT_OK;
+}
+
+View view(const ambptt_view* v) { return {v->p, v->batch, v->step, v->head}; }
+
+AttnArgs attn_args(const ambptt_attention* a) {
+  AttnArgs r{};
+  r.bf16 = a->dtype == AMBPTT_BF16;
+  r.B = a->batch, r.H = a->heads, r.G = a->group, r.dk = a->dk, r.dv = a->dv, r.T = a->steps, r.scale = a->scale;
+  return r;
+}
+
+ambptt_status check_workspace(const void* ws, size_t have, size_t need) {
+  REFUSE(need && (!ws || have < need), AMBPTT_EINVAL, "the workspace is too small");
+  REFUSE(need && misaligned(ws, 256), AMBPTT_EINVAL, "the workspace must be 256-byte aligned");
+  return AMBPTT_OK;
+}
+
+ambptt_status drop_args(const ambptt_drop* d, DropArgs* out) {
+  *out = DropArgs{0, 1.0f, 0, 0};
+  if (!d) return AMBPTT_OK;
+  REFUSE(!(d->p >= 0.0 && d->p <= 1.0), AMBPTT_EINVAL, "the dropout probability must lie in 0 .. 1");
+  const uint32_t at = uint32_t(std::nearbyint(d->p * 65536.0));
+  *out = DropArgs{at, at < 65536 ? 65536.0f / float(65536 - at) : 0.0f, d->seed, d->offset};
+  return AMBPTT_OK;
+}
+
+ambptt_status check_rows(const void* p, int64_t ld, int64_t rows, int64_t cols, int size) {
+  REFUSE(rows > 0 && !p, AMBPTT_EINVAL, "an operand is NULL");
+  REFUSE(misaligned(p, size), AMBPTT_EINVAL, "an operand is not aligned to its elements");
+  REFUSE(rows > 1 && ld < cols, AMBPTT_EINVAL, "a row stride is smaller than a row");
+  return AMBPTT_OK;
+}
+
+ambptt_status check_norm(const ambptt_norm* n) {
+  REFUSE(!n, AMBPTT_EINVAL, "norm is NULL");
+  REFUSE(!size_of(n->dtype), AMBPTT_EINVAL, "unknown dtype");
+  REFUSE(n->rows < 0 || n->cols < 1, AMBPTT_EINVAL, "need rows >= 0 and cols >= 1");
+  REFUSE(!(n->eps >= 0.0f) || !std::isfinite(n->eps), AMBPTT_EINVAL, "eps must be finite and >= 0");
+  REFUSE(n->cols > INT32_MAX, AMBPTT_EUNSUPPORTED, "cols must be below 2^31");
+  return AMBPTT_OK;
+}
+
+#define CHECK(expr)                          \
+  do {                                       \
+    const ambptt_status s_ = (expr);         \
+    if (s_ != AMBPTT_OK) return s_;          \
+  } while (0)
+
+}  // namespace
+
+extern "C" {
+
+ambptt_status ambptt_decay_attention_workspace(const ambptt_attention* a, int32_t backward, size_t* bytes) {
+  CHECK(check_attention(a));
+  REFUSE(!bytes, AMBPTT_EINVAL, "bytes is NULL");
+  *bytes = attn_workspace(attn_args(a), backward != 0);
+  return AMBPTT_OK;
+}
+
+ambptt_status ambptt_decay_attention(const ambptt_attention* a, const ambptt_view* q, const ambptt_view* k,
+                                     const ambptt_view* v, const float* log_decay, const float* s0,
+                                     const int32_t* lengths, const ambptt_view* o, float* sn, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  CHECK(check_attention(a));
+  CHECK(check_view(a, q, a->heads * a->group, a->dk, false));
+  CHECK(check_view(a, k, a->heads, a->dk, false));
+  CHECK(check_view(a, v, a->heads, a->dv, false));
+  CHECK(check_view(a, o, a->heads * a->group, a->dv, true));
+  REFUSE(!log_decay, AMBPTT_EINVAL, "log_decay is NULL");
+  REFUSE(misaligned(log_decay, 4) || misaligned(s0, 16) || misaligned(sn, 16) || misaligned(lengths, 4),
+         AMBPTT_EINVAL, "states must be aligned to 16 bytes, decays and lengths to 4");
+  AttnArgs r = attn_args(a);
+  CHECK(check_workspace(workspace, workspace_bytes, attn_workspace(r, false)));
+  r.q = view(q), r.k = view(k), r.v = view(v), r.o = view(o);
+  r.log_decay = log_decay, r.s0 = s0, r.lengths = lengths, r.sn = sn, r.ws = static_cast<char*>(workspace);
+  return done(launch_attn(r, static_cast<hipStream_t>(stream)));
+}
+
+ambptt_status ambptt_decay_attention_backward(const ambptt_attention* a, const ambptt_view* q, const ambptt_view* k,
+                                              const ambptt_view* v, const float* log_decay, const float* s0,
+                                              const int32_t* lengths, const ambptt_view* d_o, const float* dsn,
+                                              const ambptt_view* dq, const ambptt_view* dk, const ambptt_view* dv,
+                                              float* ds0, void* workspace, size_t workspace_bytes, void* stream) {
+  CHECK(check_attention(a));
+  CHECK(check_view(a, q, a->heads * a->group, a->dk, false));
+  CHECK(check_view(a, k, a->heads, a->dk, false));
+  CHECK(check_view(a, v, a->heads, a->dv, false));
+  CHECK(check_view(a, d_o, a->heads * a->group, a->dv, false));
+  CHECK(check_view(a, dq, a->heads * a->group, a->dk, true));
+  CHECK(check_view(a, dk, a->heads, a->dk, true));
+  CHECK(check_view(a, dv, a->heads, a->dv, true));
+  REFUSE(!log_decay, AMBPTT_EINVAL, "log_decay is NULL");
+  REFUSE(misaligned(log_decay, 4) || misaligned(s0, 16) || misaligned(dsn, 16) || misaligned(ds0, 16) ||
+             misaligned(lengths, 4),
+         AMBPTT_EINVAL, "states must be aligned to 16 bytes, decays and lengths to 4");
+  AttnGradArgs r{};
+  r.a = attn_args(a);
+  CHECK(check_workspace(workspace, workspace_bytes, attn_workspace(r.a, true)));
+  r.a.q = view(q), r.a.k = view(k), r.a.v = view(v), r.a.o = view(d_o);
+  r.a.log_decay = log_decay, r.a.s0 = s0, r.a.lengths = lengths, r.a.ws = static_cast<char*>(workspace);
+  r.dsn = dsn, r.dq = view(dq), r.dk = view(dk), r.dv = view(dv), r.ds0 = ds0;
+  return done(launch_attn_backward(r, static_cast<hipStream_t>(stream)));
+}
+
+ambptt_status ambptt_dropout(int32_t dtype, int64_t rows, int64_t cols, const ambptt_drop* drop, const void* x,
+                             int64_t ldx, const void* residual, int64_t ldr, void* y, int64_t ldy, void* stream) {
+  const int size = size_of(dtype);
+  REFUSE(!size, AMBPTT_EINVAL, "unknown dtype");
+  REFUSE(rows < 0 || cols < 1, AMBPTT_EINVAL, "need rows >= 0 and cols >= 1");
+  REFUSE(cols > INT32_MAX, AMBPTT_EUNSUPPORTED, "cols must be below 2^31");
+  REFUSE(!drop, AMBPTT_EINVAL, "drop is NULL");
+  DropoutArgs a{};
+  CHECK(drop_args(drop, &a.d));
+  CHECK(check_rows(x, ldx, rows, cols, size));
+  CHECK(check_rows(y, ldy, rows, cols, size));
+  if (residual) CHECK(check_rows(residual, ldr, rows, cols, size));
+  if (!rows) return AMBPTT_OK;
+  a.bf16 = dtype == AMBPTT_BF16, a.rows = rows, a.cols = cols;
+  a.x = {const_cast<void*>(x), ldx}, a.r = {const_cast<void*>(residual), ldr}, a.y = {y, ldy};
+  return done(launch_dropout(a, static_cast<hipStream_t>(stream)));
+}
+
+ambptt_status ambptt_add_norm(const ambptt_norm* n, const ambptt_drop* drop, const void* x, int64_t ldx,
+                              const void* residual, int64_t ldr, const float* w, void* h, int64_t ldh, void* y,
+                              int64_t ldy, float* scale, void* stream) {
+  CHECK(check_norm(n));
+  REFUSE(n->out != n->dtype && n->out != AMBPTT_F8, AMBPTT_EINVAL, "y is of the operands' dtype or AMBPTT_F8");
+  const bool f8 = n->out == AMBPTT_F8;
+  REFUSE(n->scale_block != 0 && (!f8 || n->scale_block != 128), AMBPTT_EINVAL,
+         "scale_block is 0 or, for 8 bits, 128");
+  REFUSE(f8 && n->rows > 0 && !scale, AMBPTT_EINVAL, "8 bits need scales");
+  const int size = size_of(n->dtype);
+  NormArgs a{};
+  CHECK(drop_args(drop, &a.d));
+  CHECK(check_rows(x, ldx, n->rows, n->cols, size));
+  CHECK(check_rows(y, ldy, n->rows, n->cols, f8 ? 1 : size));
+  if (residual) CHECK(check_rows(residual, ldr, n->rows, n->cols, size));
+  if (h) CHECK(check_rows(h, ldh, n->rows, n->cols, size));
+  REFUSE(!w || misaligned(w, 4) || misaligned(scale, 4), AMBPTT_EINVAL, "w is NULL or misaligned");
+  if (!n->rows) return AMBPTT_OK;
+  a.bf16 = n->dtype == AMBPTT_BF16, a.f8 = f8, a.block = n->scale_block, a.rows = n->rows, a.cols = int(n->cols);
+  a.eps = n->eps;
+  a.x = {const_cast<void*>(x), ldx}, a.r = {const_cast<void*>(residual), ldr}, a.h = {h, ldh}, a.y = {y, ldy};
+  a.w = w, a.scale = scale;
+  return done(launch_add_norm(a, static_cast<hipStream_t>(stream)));
+}
+
+ambptt_status ambptt_add_norm_backward_workspace(const ambptt_norm* n, size_t* bytes) {
+  CHECK(check_norm(n));
+  REFUSE(!bytes, AMBPTT_EINVAL, "bytes is NULL");
+  *bytes = size_t(norm_grad_parts(n->rows, n->cols)) * n->cols * 4;
+  return AMBPTT_OK;
+}
+
+ambptt_status ambptt_add_norm_backward(const ambptt_norm* n, const ambptt_drop* drop, const void* dy, int64_t lddy,
+                                       const void* dh, int64_t lddh, const void* h, int64_t ldh, const float* w,
+                                       void* dr, int64_t lddr, void* dx, int64_t lddx, float* dw, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+  CHECK(check_norm(n));
+  const int size = size_of(n->dtype);
+  NormGradArgs a{};
+  CHECK(drop_args(drop, &a.d));
+  CHECK(check_rows(dy, lddy, n->rows, n->cols, size));
+  CHECK(check_rows(h, ldh, n->rows, n->cols, size));
+  CHECK(check_rows(dr, lddr, n->rows, n->cols, size));
+  if (dh) CHECK(check_rows(dh, lddh, n->rows, n->cols, size));
+  if (dx) CHECK(check_rows(dx, lddx, n->rows, n->cols, size));
+  REFUSE(a.d.at && n->rows > 0 && !dx, AMBPTT_EINVAL, "dropout needs dx");
+  REFUSE(!w || misaligned(w, 4) || misaligned(dw, 4), AMBPTT_EINVAL, "w is NULL or misaligned");
+  if (dw) CHECK(check_workspace(workspace, workspace_bytes, size_t(norm_grad_parts(n->rows, n->cols)) * n->cols * 4));
+  if (!n->rows && !dw) return AMBPTT_OK;
+  a.bf16 = n->dtype == AMBPTT_BF16, a.rows = n->rows, a.cols = int(n->cols), a.eps = n->eps;
+  a.dy = {const_cast<void*>(dy), lddy}, a.dh = {const_cast<void*>(dh), lddh}, a.h = {const_cast<void*>(h), ldh};
+  a.dr = {dr, lddr}, a.dx = {dx, lddx};
+  a.w = w, a.dw = dw, a.parts = static_cast<float*>(workspace);
+  return done(launch_add_norm_backward(a, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

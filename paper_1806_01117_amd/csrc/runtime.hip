@@ -32,6 +32,7 @@
 
 #include "ambptt.h"
 #include "kernels.hpp"
+#include "ops.hpp"
 #include "resident_prog.hpp"
 #include "schedule.hpp"
 #include "tier_file.hpp"
@@ -46,6 +47,18 @@ ambptt_status fail(ambptt_status s, const std::string& msg) {
   g_err = msg;
   return s;
 }
+
+}  // namespace
+
+ambptt_status ambptt::fail_with(ambptt_status s, const char* msg) {
+  try {
+    return fail(s, msg);
+  } catch (const std::exception&) {  // no memory for the message
+    return s;
+  }
+}
+
+namespace {
 
 #define HIPCK(expr)                                                                      \
   do {                                                                                   \

@@ -1,0 +1,313 @@
+"""Python face of include/ambptt_ops.h: the operators of a residual block.
+
+Torch tensors in, torch tensors out, on the current stream of their device;
+only argument marshalling and checks of shapes, types and devices live here.
+Results are allocated by torch unless ``out`` gives a buffer for them (a dict
+with the names of the result, as ``Runner.run`` takes it).
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+from . import _lib
+from ._lib import load
+
+_torch = None
+
+
+def _t():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+def _check(status: int) -> None:
+    if status:
+        _lib.check(status)
+
+
+class _On:
+    """The device of `t` as the current one (a no-op where it is already)."""
+
+    def __init__(self, t):
+        torch = _t()
+        if t.device.type != "cuda":
+            raise ValueError(f"want cuda tensors, got {t.device}")
+        self.guard = torch.cuda.device(t.device) if t.device.index != torch.cuda.current_device() else None
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _stream(t) -> int:
+    return _t()._C._cuda_getCurrentRawStream(t.device.index)
+
+
+def _dtype(name, t) -> int:
+    torch = _t()
+    if t.dtype == torch.bfloat16:
+        return _lib.DTYPE["bf16"]
+    if t.dtype == torch.float32:
+        return _lib.DTYPE["f32"]
+    raise ValueError(f"{name}: want float32 or bfloat16, got {t.dtype}")
+
+
+def _like(name, t, shape, ref, dtype=None):
+    """`t` has the shape, and `ref`'s dtype (or `dtype`) and device."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != (dtype or ref.dtype) or t.device != ref.device:
+        raise ValueError(f"{name}: want {ref.device} {dtype or ref.dtype} {tuple(shape)}, got "
+                         f"{t.device} {t.dtype} {tuple(t.shape)}")
+    return t
+
+
+def _dense(name, t, shape, ref, dtype=None):
+    """... and is contiguous; None stays None."""
+    if t is None:
+        return None
+    _like(name, t, shape, ref, dtype)
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: want a contiguous tensor")
+    return t
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+# ---- attention ----------------------------------------------------------------
+
+
+def _view(name, t):
+    b, s, h, i = t.stride()
+    if i != 1 and t.shape[3] > 1:
+        raise ValueError(f"{name}: the elements of a head must be contiguous")
+    return C.byref(_lib.View(t.data_ptr(), b, s, h))
+
+
+def _attention(q, k, v, log_decay, lengths, scale):
+    """Checks the operands; the C struct and the sizes."""
+    torch = _t()
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        raise ValueError("q, k and v: want [batch, steps, heads, size]")
+    B, T, HQ, dk = q.shape
+    H, dv = k.shape[2], v.shape[3]
+    if H < 1 or HQ % H:
+        raise ValueError(f"{HQ} query heads do not share {H} key/value heads evenly")
+    _like("k", k, (B, T, H, dk), q)
+    _like("v", v, (B, T, H, dv), q)
+    _dense("log_decay", log_decay, (H,), q, torch.float32)
+    _dense("lengths", lengths, (B,), q, torch.int32)
+    return _lib.Attention(_dtype("q", q), B, H, HQ // H, dk, dv, T, dk ** -0.5 if scale is None else scale), \
+        (B, T, HQ, H, dk, dv)
+
+
+def _workspace(call, arg, *more, device):
+    n = C.c_size_t()
+    _check(call(C.byref(arg), *more, C.byref(n)))
+    return (_t().empty(n.value, dtype=_t().uint8, device=device) if n.value else None), n.value
+
+
+def _result(out, name, shape, ref, dtype=None):
+    """out[name], checked, or a new tensor."""
+    t = out.get(name) if out else None
+    if t is None:
+        return _t().empty(shape, dtype=dtype or ref.dtype, device=ref.device)
+    return _like(name, t, shape, ref, dtype)
+
+
+def decay_attention(q, k, v, log_decay, s0=None, lengths=None, scale=None, out: dict | None = None) -> dict:
+    """Attention whose state decays (ambptt_decay_attention): {"o", "sn"}.
+
+    q [B, T, heads * group, dk], k [B, T, heads, dk], v [B, T, heads, dv] of one
+    dtype, with any strides over batch, steps and heads; log_decay fp32 [heads];
+    s0 and the returned last state sn fp32 [B, heads, dk, dv]; lengths int32 [B].
+    With S_i = exp(log_decay) S_{i-1} + k_i v_i^T, o_i = scale S_i^T q_i (scale
+    1 / sqrt(dk) by default) for the first lengths[b] tokens of a row, and zeros
+    after them.  out["sn"] may be s0.
+    """
+    torch = _t()
+    a, (B, T, HQ, H, dk, dv) = _attention(q, k, v, log_decay, lengths, scale)
+    with _On(q):
+        state = (B, H, dk, dv)
+        _dense("s0", s0, state, q, torch.float32)
+        o = _result(out, "o", (B, T, HQ, dv), q)
+        sn = _dense("sn", _result(out, "sn", state, q, torch.float32), state, q, torch.float32)
+        L = load()
+        ws, n = _workspace(L.ambptt_decay_attention_workspace, a, 0, device=q.device)
+        _check(L.ambptt_decay_attention(C.byref(a), _view("q", q), _view("k", k), _view("v", v), _ptr(log_decay),
+                                        _ptr(s0), _ptr(lengths), _view("o", o), _ptr(sn), _ptr(ws), n, _stream(q)))
+    return {"o": o, "sn": sn}
+
+
+def decay_attention_step(q, k, v, log_decay, s, lengths=None, scale=None, out=None):
+    """One token for each row, the state `s` advanced in place: returns o.
+
+    q [B, 1, heads * group, dk] and so on as in decay_attention; a row with
+    lengths[b] = 0 sits out (its state stays, its output is zero).
+    """
+    if s is None:
+        raise ValueError("s: a generator's step needs its state")
+    if q.dim() != 4 or q.shape[1] != 1:
+        raise ValueError("q: want one token, [batch, 1, heads, size]")
+    return decay_attention(q, k, v, log_decay, s0=s, lengths=lengths, scale=scale,
+                           out={"sn": s} if out is None else {"sn": s, "o": out})["o"]
+
+
+def decay_attention_backward(q, k, v, log_decay, do, s0=None, dsn=None, lengths=None, scale=None,
+                             out: dict | None = None) -> dict:
+    """Gradients of decay_attention (ambptt_decay_attention_backward).
+
+    {"dq", "dk", "dv", "ds0"} from do (of o) and dsn (of sn, None: zeros); ds0
+    where s0 or dsn was given (or out["ds0"]), else None.
+    """
+    torch = _t()
+    a, (B, T, HQ, H, dk, dv) = _attention(q, k, v, log_decay, lengths, scale)
+    with _On(q):
+        state = (B, H, dk, dv)
+        _dense("s0", s0, state, q, torch.float32)
+        _dense("dsn", dsn, state, q, torch.float32)
+        _like("do", do, (B, T, HQ, dv), q)
+        res = {"dq": _result(out, "dq", q.shape, q), "dk": _result(out, "dk", k.shape, q),
+               "dv": _result(out, "dv", v.shape, q), "ds0": None}
+        if s0 is not None or dsn is not None or (out and out.get("ds0") is not None):
+            res["ds0"] = _dense("ds0", _result(out, "ds0", state, q, torch.float32), state, q, torch.float32)
+        L = load()
+        ws, n = _workspace(L.ambptt_decay_attention_workspace, a, 1, device=q.device)
+        _check(L.ambptt_decay_attention_backward(
+            C.byref(a), _view("q", q), _view("k", k), _view("v", v), _ptr(log_decay), _ptr(s0), _ptr(lengths),
+            _view("do", do), _ptr(dsn), _view("dq", res["dq"]), _view("dk", res["dk"]), _view("dv", res["dv"]),
+            _ptr(res["ds0"]), _ptr(ws), n, _stream(q)))
+    return res
+
+
+# ---- dropout and norm -----------------------------------------------------------
+
+
+def _rows(name, t):
+    """(pointer, row stride) of a tensor seen as rows of its last dimension."""
+    shape, stride = t.shape, t.stride()
+    if shape[-1] > 1 and stride[-1] != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    if len(shape) == 1:
+        return t.data_ptr(), shape[-1]
+    ld, over = None, 1
+    for n, st in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+        if n != 1:
+            if ld is None:
+                ld = st
+            elif st != ld * over:
+                raise ValueError(f"{name}: the rows have no common stride")
+            over *= n
+    return t.data_ptr(), shape[-1] if ld is None else ld
+
+
+def _sizes(name, x):
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError(f"{name}: want rows of one element and more")
+    cols = x.shape[-1]
+    return x.numel() // cols, cols
+
+
+def _drop(p, seed, offset):
+    """The C struct, or None without dropout (a p that rounds to no 65536th keeps all)."""
+    if p == 0.0:
+        return None
+    return C.byref(_lib.Drop(p, seed & 0xFFFFFFFFFFFFFFFF, offset & 0xFFFFFFFFFFFFFFFF))
+
+
+def dropout(x, p, seed, offset=0, residual=None, out=None):
+    """residual + dropout(x) (ambptt_dropout); without residual, of a gradient: dropout's gradient.
+
+    The mask is a function of (seed, offset, row, column) alone, rows being
+    those of the last dimension: the same numbers give the same mask wherever a
+    step is evaluated again.  A call uses dropout_counters(x) counters from
+    `offset`.  `out` may be x or residual.
+    """
+    dt = _dtype("x", x)
+    rows, cols = _sizes("x", x)
+    with _On(x):
+        if residual is not None:
+            _like("residual", residual, x.shape, x)
+        y = _result({"out": out}, "out", x.shape, x)
+        xp, xl = _rows("x", x)
+        rp, rl = _rows("residual", residual) if residual is not None else (None, 0)
+        yp, yl = _rows("out", y)
+        _check(load().ambptt_dropout(dt, rows, cols, C.byref(_lib.Drop(p, seed & 0xFFFFFFFFFFFFFFFF,
+                                                                       offset & 0xFFFFFFFFFFFFFFFF)),
+                                     xp, xl, rp, rl, yp, yl, _stream(x)))
+    return y
+
+
+def dropout_counters(x) -> int:
+    """Counters that dropout of a tensor of x's shape uses: the next call's offset is that much further."""
+    rows, cols = _sizes("x", x)
+    return rows * -(-cols // 8)
+
+
+def add_norm(x, w, residual=None, eps=1e-6, p=0.0, seed=0, offset=0, out_dtype=None, scale_block=0,
+             out: dict | None = None) -> dict:
+    """h = residual + dropout(x), y = w h / sqrt(mean(h^2) + eps) (ambptt_add_norm): {"h", "y"}.
+
+    Rows are those of the last dimension; w fp32 [cols].  out_dtype "f8": y is
+    torch.float8_e4m3fn with "scale" fp32 [..., n] beside it, n = 1 scale per row
+    or, with scale_block 128, one per 128 columns; y times its scale is the value.
+    """
+    torch = _t()
+    if out_dtype not in (None, "f8"):
+        raise ValueError('out_dtype: want None or "f8"')
+    rows, cols = _sizes("x", x)
+    f8 = out_dtype == "f8"
+    dt = _dtype("x", x)
+    a = _lib.Norm(dt, _lib.F8 if f8 else dt, rows, cols, scale_block, eps)
+    with _On(x):
+        if residual is not None:
+            _like("residual", residual, x.shape, x)
+        _dense("w", w, (cols,), x, torch.float32)
+        h = _result(out, "h", x.shape, x)
+        y = _result(out, "y", x.shape, x, torch.float8_e4m3fn if f8 else None)
+        res = {"h": h, "y": y}
+        if f8:
+            shape = (*x.shape[:-1], -(-cols // scale_block) if scale_block > 0 else 1)
+            res["scale"] = _dense("scale", _result(out, "scale", shape, x, torch.float32), shape, x, torch.float32)
+        _check(load().ambptt_add_norm(C.byref(a), _drop(p, seed, offset), *_rows("x", x),
+                                      *(_rows("residual", residual) if residual is not None else (None, 0)),
+                                      _ptr(w), *_rows("h", h), *_rows("y", y), _ptr(res.get("scale")), _stream(x)))
+    return res
+
+
+def add_norm_backward(dy, h, w, dh=None, eps=1e-6, p=0.0, seed=0, offset=0, out: dict | None = None) -> dict:
+    """Gradients of add_norm (ambptt_add_norm_backward): {"dresidual", "dw"}, and "dx" where p > 0.
+
+    dy of y, dh of h (None: zeros), h as add_norm returned it.  Without dropout
+    x's gradient is the residual's.
+    """
+    torch = _t()
+    rows, cols = _sizes("h", h)
+    dt = _dtype("h", h)
+    a = _lib.Norm(dt, dt, rows, cols, 0, eps)
+    with _On(h):
+        _like("dy", dy, h.shape, h)
+        if dh is not None:
+            _like("dh", dh, h.shape, h)
+        _dense("w", w, (cols,), h, torch.float32)
+        drop = _drop(p, seed, offset)
+        dr = _result(out, "dresidual", h.shape, h)
+        dx = _result(out, "dx", h.shape, h) if drop is not None else None
+        dw = _dense("dw", _result(out, "dw", (cols,), h, torch.float32), (cols,), h, torch.float32)
+        L = load()
+        ws, n = _workspace(L.ambptt_add_norm_backward_workspace, a, device=h.device)
+        _check(L.ambptt_add_norm_backward(
+            C.byref(a), drop, *_rows("dy", dy), *(_rows("dh", dh) if dh is not None else (None, 0)), *_rows("h", h),
+            _ptr(w), *_rows("dresidual", dr), *(_rows("dx", dx) if dx is not None else (None, 0)), _ptr(dw), _ptr(ws),
+            n, _stream(h)))
+    res = {"dresidual": dr, "dw": dw}
+    if dx is not None:
+        res["dx"] = dx
+    return res

@@ -1,0 +1,185 @@
+"""Pins of the float64 operators (decayed attention, dropout, norm) on the CPU,
+and the refusals of their C entries, which need no GPU."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from oracle import ops as O
+
+
+def _differences(f, x, h=1e-6):
+    """Central differences of the scalar f at x, entry by entry."""
+    g = np.zeros_like(x)
+    for i in np.ndindex(x.shape):
+        y = x.copy()
+        y[i] += h
+        up = f(y)
+        y[i] -= 2 * h
+        g[i] = (up - f(y)) / (2 * h)
+    return g
+
+
+@pytest.mark.parametrize("G,lengths", [(1, None), (2, [3, 0]), (3, [1, 4])])
+def test_attention_gradients_against_differences(G, lengths):
+    r = np.random.default_rng(1)
+    B, T, H, a, e = 2, 4, 2, 3, 2
+    x = {"q": r.normal(size=(B, T, H * G, a)), "k": r.normal(size=(B, T, H, a)), "v": r.normal(size=(B, T, H, e)),
+         "s0": r.normal(size=(B, H, a, e))}
+    g = np.array([-0.3, 0.0])
+    do, dsn = r.normal(size=(B, T, H * G, e)), r.normal(size=(B, H, a, e))
+
+    def loss(**kw):
+        y = {**x, **kw}
+        o, sn = O.attention(y["q"], y["k"], y["v"], g, y["s0"], lengths, 0.7)
+        return (o * do).sum() + (sn * dsn).sum()
+
+    got = O.attention_backward(x["q"], x["k"], x["v"], g, do, x["s0"], dsn, lengths, 0.7)
+    for name, have in zip(("q", "k", "v", "s0"), got):
+        want = _differences(lambda y: loss(**{name: y}), x[name])
+        assert np.abs(have - want).max() <= 1e-7 * max(1.0, np.abs(want).max()), name
+
+
+def test_attention_equals_its_sum():
+    # o_i = scale (sum_{j <= i} lam^(i-j) (q_i . k_j) v_j + lam^(i+1) s0^T q_i)
+    r = np.random.default_rng(2)
+    T, a, e, lam = 5, 4, 3, 0.8
+    q, k, v, s0 = r.normal(size=(T, a)), r.normal(size=(T, a)), r.normal(size=(T, e)), r.normal(size=(a, e))
+    o, sn = O.attention(q[None, :, None], k[None, :, None], v[None, :, None], [np.log(lam)], s0[None, None])
+    for i in range(T):
+        want = lam ** (i + 1) * q[i] @ s0 + sum(lam ** (i - j) * (q[i] @ k[j]) * v[j] for j in range(i + 1))
+        assert np.allclose(o[0, i, 0], want, rtol=1e-13)
+    want = lam ** T * s0 + sum(lam ** (T - 1 - j) * np.outer(k[j], v[j]) for j in range(T))
+    assert np.allclose(sn[0, 0], want, rtol=1e-13)
+
+
+def test_philox_known_answers():
+    # the test vectors published with the generator
+    assert O.philox((0, 0, 0, 0), (0, 0)) == [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]
+    m = 0xFFFFFFFF
+    assert O.philox((m, m, m, m), (m, m)) == [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]
+
+
+@pytest.mark.parametrize("p", [0.1, 0.5, 0.9])
+def test_dropout_keeps_its_share(p):
+    f = O.dropout_factors(64, 203, p, 12345, 1 << 40)
+    n, kept = f.size, (f > 0).mean()
+    assert abs(kept - (1 - p)) <= 5 * np.sqrt(p * (1 - p) / n)
+    assert abs(f.mean() - 1.0) <= 5 * np.sqrt(p / (1 - p) / n)
+    assert (O.dropout_factors(3, 20, 0.0, 1, 0) == 1.0).all() and (O.dropout_factors(3, 20, 1.0, 1, 0) == 0.0).all()
+
+
+def test_norm_gradients_against_differences():
+    r = np.random.default_rng(3)
+    h, w, dy, dh = r.normal(size=(3, 5)), r.normal(size=5), r.normal(size=(3, 5)), r.normal(size=(3, 5))
+    dr, dw = O.norm_backward(dy, h, w, dh, 1e-3)
+    assert np.allclose(dr, _differences(lambda y: (O.norm(y, w, 1e-3) * dy).sum() + (y * dh).sum(), h), atol=1e-8)
+    assert np.allclose(dw, _differences(lambda y: (O.norm(h, y, 1e-3) * dy).sum(), w), atol=1e-8)
+
+
+# ---- refusals: nothing is enqueued, so no GPU is needed -------------------------
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_1806_01117_amd as amb
+    return amb.load()
+
+
+EINVAL, EUNSUPPORTED = -1, -4
+GOOD = dict(dtype=0, batch=2, heads=3, group=2, dk=64, dv=48, steps=10, scale=0.125)
+
+
+def _attention(lib, change=None, views=None, **ptr):
+    from paper_1806_01117_amd import _lib
+    a = _lib.Attention(**{**GOOD, **(change or {})})
+    n = ctypes.c_size_t()
+    st = lib.ambptt_decay_attention_workspace(ctypes.byref(a), 0, ctypes.byref(n))
+    if st:
+        return st
+    v = {n: dict(p=4096, batch=100000, step=1000, head=128) for n in "qkvo"}
+    for name, more in (views or {}).items():
+        v[name].update(more)
+    v = {n: ctypes.byref(_lib.View(**x)) for n, x in v.items()}
+    p = {"log_decay": 4096, "s0": 4096, "lengths": 4096, "sn": 4096, "ws": 4096, "ws_bytes": n.value, **ptr}
+    return lib.ambptt_decay_attention(ctypes.byref(a), v["q"], v["k"], v["v"], p["log_decay"], p["s0"], p["lengths"],
+                                      v["o"], p["sn"], p["ws"], p["ws_bytes"], None)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=2), EINVAL), (dict(batch=0), EINVAL), (dict(heads=0), EINVAL), (dict(group=0), EINVAL),
+    (dict(dk=0), EINVAL), (dict(steps=-1), EINVAL), (dict(scale=float("nan")), EINVAL), (dict(dk=24), EUNSUPPORTED),
+    (dict(dv=144), EUNSUPPORTED), (dict(steps=2 ** 31), EUNSUPPORTED), (dict(batch=2 ** 24), EUNSUPPORTED),
+])
+def test_attention_refuses_sizes(lib, change, status):
+    assert _attention(lib, change) == status
+    assert lib.ambptt_last_error()
+
+
+@pytest.mark.parametrize("views,ptr", [
+    (dict(q=dict(p=None)), {}), (dict(k=dict(step=-8)), {}), (dict(v=dict(p=4097)), {}), (dict(o=dict(head=0)), {}),
+    (dict(o=dict(step=47)), {}), (dict(o=dict(batch=0)), {}), ({}, dict(log_decay=None)), ({}, dict(s0=4100)),
+    ({}, dict(sn=4104)), ({}, dict(lengths=4098)),
+])
+def test_attention_refuses_operands(lib, views, ptr):
+    assert _attention(lib, None, views, **ptr) == EINVAL
+
+
+def test_attention_refuses_null(lib):
+    n = ctypes.c_size_t()
+    assert lib.ambptt_decay_attention_workspace(None, 0, ctypes.byref(n)) == EINVAL
+    from paper_1806_01117_amd import _lib
+    a = _lib.Attention(**GOOD)
+    assert lib.ambptt_decay_attention_workspace(ctypes.byref(a), 0, None) == EINVAL
+
+
+def _norm(lib, drop=None, **kw):
+    from paper_1806_01117_amd import _lib
+    d = dict(dtype=1, out=1, rows=4, cols=100, scale_block=0, eps=1e-6, x=4096, ldx=100, r=None, ldr=0, w=4096, h=4096,
+             ldh=100, y=4096, ldy=100, scale=None)
+    d.update(kw)
+    a = _lib.Norm(*(d[k] for k in ("dtype", "out", "rows", "cols", "scale_block", "eps")))
+    drop = ctypes.byref(_lib.Drop(*drop)) if drop else None
+    return lib.ambptt_add_norm(ctypes.byref(a), drop, d["x"], d["ldx"], d["r"], d["ldr"], d["w"], d["h"], d["ldh"],
+                               d["y"], d["ldy"], d["scale"], None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dtype=7), dict(out=0), dict(rows=-1), dict(cols=0), dict(eps=-1.0), dict(eps=float("inf")), dict(scale_block=128),
+    dict(out=2), dict(out=2, scale=4096, scale_block=64), dict(x=None), dict(x=4097), dict(ldx=99), dict(w=None),
+    dict(w=4098), dict(r=4096, ldr=3), dict(drop=(1.5, 0, 0)), dict(drop=(float("nan"), 0, 0)),
+])
+def test_norm_refuses(lib, kw):
+    assert _norm(lib, **kw) == EINVAL
+
+
+def test_norm_without_rows_is_done(lib):
+    assert _norm(lib, rows=0, x=None, y=None, h=None) == 0
+
+
+def test_norm_backward_refuses(lib):
+    from paper_1806_01117_amd import _lib
+    a = _lib.Norm(0, 0, 4, 100, 0, 1e-6)
+    n = ctypes.c_size_t()
+    assert lib.ambptt_add_norm_backward_workspace(ctypes.byref(a), ctypes.byref(n)) == 0 and n.value > 0
+
+    def call(drop=None, dx=None, dw=4096, ws=4096, have=n.value, dr=4096):
+        return lib.ambptt_add_norm_backward(ctypes.byref(a), drop, 4096, 100, None, 0, 4096, 100, 4096, dr, 100, dx, 100,
+                                            dw, ws, have, None)
+
+    assert call(have=n.value - 4) == EINVAL and call(ws=None) == EINVAL and call(ws=4100) == EINVAL
+    assert call(dr=None) == EINVAL and call(drop=ctypes.byref(_lib.Drop(0.5, 1, 2))) == EINVAL
+
+
+def test_dropout_refuses(lib):
+    from paper_1806_01117_amd import _lib
+
+    def call(dtype=0, rows=4, cols=100, p=0.5, x=4096, ldx=100, y=4096, ldy=100, drop=True):
+        d = ctypes.byref(_lib.Drop(p, 1, 2)) if drop else None
+        return lib.ambptt_dropout(dtype, rows, cols, d, x, ldx, None, 0, y, ldy, None)
+
+    for kw in (dict(dtype=2), dict(rows=-1), dict(cols=0), dict(p=-0.1), dict(p=1.1), dict(x=None), dict(y=4098),
+               dict(ldx=50), dict(drop=False)):
+        assert call(**kw) == EINVAL, kw
+    assert call(rows=0, x=None, y=None) == 0
+    assert call(cols=2 ** 31, ldx=2 ** 31, ldy=2 ** 31) == EUNSUPPORTED
