@@ -53,7 +53,8 @@ typedef struct {
 
 /* A [batch][steps][heads][size] operand anywhere in memory: element (b, t, h, i)
  * is at p[b * batch + t * step + h * head + i], strides in elements, >= 0
- * (zero strides broadcast an input; an output's elements must not overlap). */
+ * (zero strides broadcast an input; an output's elements must not overlap).
+ * EUNSUPPORTED for tokens more than 2^28 bytes apart. */
 typedef struct {
   void* p;
   int64_t batch, step, head;

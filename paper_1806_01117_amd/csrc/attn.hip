@@ -13,13 +13,20 @@
 // segment's own contribution to the state, a second one passes the states from
 // segment to segment, and the segments then run side by side.
 //
+// Split.  Wave w of a workgroup holds the columns 16 w .. of the state, all its
+// rows, and forms those columns of the results.  Its accumulators are then
+// operands of the product with q as they stand, and nothing of the state passes
+// through LDS; the products q k^T are shared out over the waves and exchanged
+// there.
+//
 // Rounding.  States, accumulators and sums are fp32, and bf16 operands enter
 // the matrix cores as they are.  The fp32 values that go there in the bf16
 // kernels are split in bf16 parts: the weighted products lambda^(i-j) (q_i . k_j)
 // and the copy of the state that multiplies q in two (16 bits; with one part
 // each a result was 1.35 times as far off as its own rounding to bf16 makes
-// it), the weighted rows lambda^(m-1-j) k_j, which go into the fp32 state, in
-// three (24 bits).
+// it), the weighted rows lambda^(m-1-j) k_j in three (24 bits) where the state
+// itself is a result, and in two (2.8e-6 of each) where it only goes into
+// results that are bf16.
 #include "mfma.hpp"
 #include "ops.hpp"
 
@@ -27,13 +34,8 @@ namespace ambptt {
 
 namespace {
 
-constexpr int kC = 64;    // tokens per chunk: 16 rows for each of 4 pairs of waves
-constexpr int kPad = 16;  // bytes between rows in LDS: 16 rows start in different banks
-
-// Eight waves: wave w has the rows of w % 4, and of the state and the results
-// the half w / 4 (backwards: dv or dk), so that its accumulators and fragments
-// fit in 256 registers and two waves share a SIMD.
-constexpr int kThreads = 512, kSets = 2;
+constexpr int kC = 64;          // tokens per chunk
+constexpr int kRows = kC / 16;  // ... in tiles of 16
 
 typedef unsigned int u4v __attribute__((ext_vector_type(4)));
 typedef unsigned int u2v __attribute__((ext_vector_type(2)));
@@ -50,6 +52,20 @@ __device__ __forceinline__ unsigned pk_bf16(float a, float b) {
 }
 __device__ __forceinline__ float lo_f(unsigned p) { return __builtin_bit_cast(float, p << 16); }
 __device__ __forceinline__ float hi_f(unsigned p) { return __builtin_bit_cast(float, p & 0xffff0000u); }
+// x minus the low (the high) value of a pair, exactly where the pair rounded x:
+// a product of pairs with (-1, 0) or (0, -1), one instruction where unpacking
+// and subtracting take two.  The factors come from a register: written as the
+// constant -1.0 the pair (-1, 0) reaches the instruction as (0, -1).
+__device__ __forceinline__ float less_lo(float x, unsigned p) {
+  unsigned f = 0x0000bf80u;
+  asm("" : "+s"(f));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p), __builtin_bit_cast(bf16x2, f), x, false);
+}
+__device__ __forceinline__ float less_hi(float x, unsigned p) {
+  unsigned f = 0xbf800000u;
+  asm("" : "+s"(f));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p), __builtin_bit_cast(bf16x2, f), x, false);
+}
 
 // Fragments of 16 x 16 tiles.  A lane l of a wave stands for row (or column)
 // l % 16 and for the group l / 16 of the reduction's indices.
@@ -59,6 +75,56 @@ __device__ __forceinline__ float hi_f(unsigned p) { return __builtin_bit_cast(fl
 // tile in LDS: a unit is kTiles tiles of 16 rows, and slot (tile, r) of group g
 // is row 16 tile + 4 g + r, which is where a product's accumulators lie, so
 // that the weighted products are operands of the next product as they stand.
+// Rows lie in LDS without gaps, their 16-byte pieces permuted by an XOR with
+// twist(row).  One clock serves 256 bytes: of a 16-byte read the lanes 0-3,
+// 12-15 and 20-27 (then the others of 32), of an 8-byte read 32 lanes.  So that
+// those meet all 64 banks once, the twists of rows 0-7, and those of 8-15,
+// differ without their lowest bit (token fragments: two pieces of eight rows),
+// and rows 4-11 have each other's with that bit flipped (row fragments: one
+// piece of 16 rows, piece g of lanes 16 g ..).
+template <class T, int NX>
+__device__ __forceinline__ int twist(int row) {
+  if constexpr (sizeof(T) == 4) return row & 15;
+  if constexpr (NX == 64) return (((row >> 1) ^ (row >> 2 & 2)) & 3) << 1 | (row >> 3 & 1);  // two rows to all banks
+  return ((row ^ (row >> 1 & 4)) & 7) << 1 | (row >> 3 & 1);
+}
+template <class T, int NX>
+constexpr int tile_ld = NX* int(sizeof(T));  // bytes of a row
+// byte offset of column byte `col`; flipping bits of `col` above the lowest 16
+// values flips the same bits of the offset
+template <class T, int NX>
+__device__ __forceinline__ int tile_at(int row, int col) {
+  return row * tile_ld<T, NX> + (((col >> 4) ^ twist<T, NX>(row)) << 4) + (col & 15);
+}
+// LDS by its 32-bit addresses, so that a lane keeps one register for an address
+// and the rest of it is in the instruction
+template <class V>
+__device__ __forceinline__ V get(unsigned at) {
+  return *(__attribute__((address_space(3))) const V*)at;
+}
+template <class V>
+__device__ __forceinline__ void put(unsigned at, const V& v) {
+  *(__attribute__((address_space(3))) V*)at = v;
+}
+// a lane's value as one that a loop does not know, so that it keeps no sums of it
+__device__ __forceinline__ unsigned here(unsigned v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+// ... and an address in memory that all lanes share, so that it stays in scalar registers
+typedef __attribute__((address_space(1))) char* Global;
+__device__ __forceinline__ Global shared_here(const void* p) {
+  asm volatile("" : "+s"(p));
+  return (Global)(uint64_t)p;
+}
+// a lane's address, flipped: formed where it is used, so that a loop does not
+// keep a register for each flip
+__device__ __forceinline__ unsigned flip(unsigned at, int bits) {
+  if (bits == 0) return at;
+  asm volatile("" : "+s"(bits));
+  return at ^ bits;
+}
+
 template <class T>
 struct Mm;
 
@@ -67,23 +133,29 @@ struct Mm<__bf16> {
   typedef bf16x8 Frag;
   static constexpr int kTiles = 2, kParts = 3, kHalves = 2;
   static __device__ __forceinline__ f4 mul(const Frag& a, const Frag& b, f4 c) { return mfma_bf16_16x16x32(a, b, c); }
-  // column of lane n in tile t: two tiles share 32 columns so that a lane's
-  // accumulators of both are 8 neighbours (16 bytes to store)
-  static __device__ __forceinline__ int column(int t, int n) { return 32 * (t / 2) + 8 * (n / 4) + 4 * (t % 2) + n % 4; }
-  // token fragment of unit u for the columns that `lane` points at (token_lane)
-  static __device__ __forceinline__ Frag token(const char* lane, int ld, int u) {
+  // the row of the state at accumulator r of tile t: two tiles share 32 rows so
+  // that a lane's accumulators of both are 8 neighbours, a row fragment's order
+  static __device__ __forceinline__ int row(int t, int r) { return 32 * (t / 2) + 8 * (threadIdx.x % 64 / 16) + 4 * (t % 2) + r; }
+  // token fragment of unit u from a lane's address (token_at): 16 lanes read 4
+  // rows of 16 columns, 4 columns each, and get them transposed
+  static __device__ __forceinline__ Frag token(unsigned at, int ld, int u) {
     typedef __attribute__((address_space(3))) bf16x4* Lds;
-    const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((Lds)(lane + 32 * u * ld));
-    const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((Lds)(lane + (32 * u + 16) * ld));
+    const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((Lds)(at + 32 * u * ld));
+    const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((Lds)(at + (32 * u + 16) * ld));
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
   }
-  // a lane's address for token(): 16 lanes read 4 rows of 16 columns, 4 columns
-  // each, and get them transposed
-  static __device__ __forceinline__ const char* token_lane(const char* tile, int ld, int l) {
-    return tile + (4 * (l / 16) + l % 16 / 4) * ld;
+  // ... for the columns 16 t ..
+  template <int NX>
+  static __device__ __forceinline__ int token_at(int l, int t) {
+    return tile_at<__bf16, NX>(4 * (l / 16) + l % 16 / 4, 2 * (16 * t + 4 * (l % 4)));
   }
-  static __device__ __forceinline__ int token_col(int t, int l) { return 2 * (32 * (t / 2) + 8 * (l % 4) + 4 * (t % 2)); }
-  static __device__ __forceinline__ int token_plain_col(int t, int l) { return 2 * (16 * t + 4 * (l % 4)); }
+  // ... and for the columns that are the rows row(t, .) of the state, from that for t = 0
+  template <int NX>
+  static __device__ __forceinline__ int state_at() {
+    const int l = threadIdx.x % 64;
+    return tile_at<__bf16, NX>(4 * (l / 16) + l % 16 / 4, 2 * (8 * (l % 4)));
+  }
+  static __device__ __forceinline__ unsigned state_tile(unsigned at, int t) { return flip(at, 64 * (t / 2)) + 8 * (t % 2); }
   // accumulators of kTiles tiles as token fragments, in kHalves parts
   static __device__ __forceinline__ void pack(const f4 (&p)[2], Frag (&out)[2]) {
     u4v a, b;
@@ -91,32 +163,27 @@ struct Mm<__bf16> {
     for (int i = 0; i < 4; ++i) {
       const float x = p[i / 2][i % 2 * 2], y = p[i / 2][i % 2 * 2 + 1];
       a[i] = pk_bf16(x, y);
-      b[i] = pk_bf16(x - lo_f(a[i]), y - hi_f(a[i]));
+      b[i] = pk_bf16(less_lo(x, a[i]), less_hi(y, a[i]));
     }
     out[0] = __builtin_bit_cast(Frag, a), out[1] = __builtin_bit_cast(Frag, b);
   }
-  // x times the weights, in kParts parts whose sum is exact to 24 bits
-  static __device__ __forceinline__ void split(const Frag& x, const float (&w)[8], Frag (&out)[kParts]) {
+  // x times the weights, in parts of 8 bits: three hold all of them
+  template <int PARTS>
+  static __device__ __forceinline__ void split(const Frag& x, const float (&w)[8], Frag (&out)[PARTS]) {
     const u4v v = __builtin_bit_cast(u4v, x);
-    u4v o[kParts];
+    u4v o[PARTS];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float a = lo_f(v[i]) * w[2 * i], b = hi_f(v[i]) * w[2 * i + 1];
 #pragma unroll
-      for (int p = 0; p < kParts; ++p) {
+      for (int p = 0; p < PARTS; ++p) {
         const unsigned q = pk_bf16(a, b);
         o[p][i] = q;
-        a -= lo_f(q), b -= hi_f(q);
+        if (p + 1 < PARTS) a = less_lo(a, q), b = less_hi(b, q);
       }
     }
 #pragma unroll
-    for (int p = 0; p < kParts; ++p) out[p] = __builtin_bit_cast(Frag, o[p]);
-  }
-  // four accumulators as elements, their parts `apart` bytes from each other
-  static __device__ __forceinline__ void put4(char* p, int apart, const f4& v) {
-    const u2v a = {pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
-    *(u2v*)p = a;
-    *(u2v*)(p + apart) = u2v{pk_bf16(v[0] - lo_f(a[0]), v[1] - hi_f(a[0])), pk_bf16(v[2] - lo_f(a[1]), v[3] - hi_f(a[1]))};
+    for (int p = 0; p < PARTS; ++p) out[p] = __builtin_bit_cast(Frag, o[p]);
   }
 };
 
@@ -130,70 +197,68 @@ struct Mm<float> {
     asm volatile("" ::: "memory");  // loads stay where they are: hoisted, they would spill
     return c;
   }
-  static __device__ __forceinline__ int column(int t, int n) { return 16 * t + n; }
-  static __device__ __forceinline__ Frag token(const char* lane, int ld, int u) {
+  static __device__ __forceinline__ int row(int t, int r) { return 16 * t + 4 * (threadIdx.x % 64 / 16) + r; }
+  // row 4 g + r of a lane's four: its twist is that of 4 g with r in the low bits
+  static __device__ __forceinline__ Frag token(unsigned at, int ld, int u) {
     f4 v;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = *(const float*)(lane + (16 * u + r) * ld);
+    for (int r = 0; r < 4; ++r) v[r] = get<float>((at ^ (r << 4)) + (16 * u + r) * ld);
     return v;
   }
-  static __device__ __forceinline__ const char* token_lane(const char* tile, int ld, int l) { return tile + 4 * (l / 16) * ld; }
-  static __device__ __forceinline__ int token_col(int t, int l) { return 4 * (16 * t + l % 16); }
-  static __device__ __forceinline__ int token_plain_col(int t, int l) { return 4 * (16 * t + l % 16); }
+  template <int NX>
+  static __device__ __forceinline__ int token_at(int l, int t) {
+    return tile_at<float, NX>(4 * (l / 16), 4 * (16 * t + l % 16));
+  }
+  template <int NX>
+  static __device__ __forceinline__ int state_at() {
+    return token_at<NX>(threadIdx.x % 64, 0);
+  }
+  static __device__ __forceinline__ unsigned state_tile(unsigned at, int t) { return flip(at, 64 * t); }
   static __device__ __forceinline__ void pack(const f4 (&p)[1], Frag (&out)[1]) { out[0] = p[0]; }
   static __device__ __forceinline__ void split(const Frag& x, const float (&w)[4], Frag (&out)[1]) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) out[0][r] = x[r] * w[r];
   }
-  static __device__ __forceinline__ void put4(char* p, int, const f4& v) { *(f4*)p = v; }
 };
 
 // 64 rows of NX elements on their way from memory to LDS
-template <class T, int NX>
-constexpr int tile_ld = NX* int(sizeof(T)) + kPad;  // bytes of a row in LDS
-
-template <class T, int NX>
+template <class T, int NX, int THREADS>
 struct Stage {
-  static constexpr int kLd = tile_ld<T, NX>;
-  static constexpr int kLanes = NX * int(sizeof(T)) / 16;  // lanes per row
-  static constexpr int kPer = kThreads / kLanes;           // rows per load
-  static constexpr int kLoads = kC / kPer;
+  static constexpr int kSize = int(sizeof(T)), kLanes = NX * kSize / 16;  // lanes per row
+  static constexpr int kWaveRows = 64 / kLanes;                           // rows of a wave's load
+  static constexpr int kPer = THREADS / kLanes, kLoads = kC / kPer;       // rows of a load by all
   u4v v[kLoads];
+  __device__ __forceinline__ static int col(int id) { return id % kLanes * (16 / kSize); }
   // rows 0 .. m - 1 at p with the row stride `step` (elements), nx of their NX columns; the rest are zeros
   __device__ __forceinline__ void load(const T* p, int64_t step, int m, int nx) {
-    const int row = threadIdx.x / kLanes, col = threadIdx.x % kLanes * (16 / int(sizeof(T)));
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const unsigned id = here(threadIdx.x);
+    const char* const first = reinterpret_cast<const char*>(p + wave * kWaveRows * step);  // a wave's first row
+    const unsigned from = (id % 64 / kLanes * unsigned(step) + col(id)) * kSize;
+    const bool whole = m == kC && nx == NX;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int r = row + i * kPer;
-      v[i] = r < m && col < nx ? *(const u4u*)(p + r * step + col) : u4v{0, 0, 0, 0};
+      typedef __attribute__((address_space(1))) const u4u* Piece;
+      const Global at = shared_here(first + i * kPer * step * kSize);
+      if (whole)
+        v[i] = *(Piece)(at + from);
+      else
+        v[i] = int(id / kLanes) + i * kPer < m && col(id) < nx ? *(Piece)(at + from) : u4v{0, 0, 0, 0};
     }
   }
-  __device__ __forceinline__ void put(char* lds) const {
-    const int row = threadIdx.x / kLanes, at = threadIdx.x % kLanes * 16;
+  // this thread's first address in a tile; the rows that follow are multiples of 16 further or have their own
+  static __device__ __forceinline__ int put_at(unsigned id, int i) { return tile_at<T, NX>(id / kLanes + i * kPer, id % kLanes * 16); }
+  __device__ __forceinline__ void to(unsigned tile) const {
+    const unsigned id = here(threadIdx.x);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) *(u4v*)(lds + (row + i * kPer) * kLd + at) = v[i];
-  }
-};
-
-// row fragments of one row (zeros for a row that is not there)
-template <class T, int NX>
-struct RowFrags {
-  static constexpr int kUnits = NX * int(sizeof(T)) / 64;
-  typename Mm<T>::Frag f[kUnits];
-  __device__ __forceinline__ void load(const T* row, bool there, int nx) {
-    const int g = threadIdx.x % 64 / 16;
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const int col = (u * 64 + g * 16) / int(sizeof(T));
-      const u4v v = there && col < nx ? *(const u4u*)(row + col) : u4v{0, 0, 0, 0};
-      f[u] = __builtin_bit_cast(typename Mm<T>::Frag, v);
-    }
+    for (int i = 0; i < kLoads; ++i) put(kPer % 16 == 0 ? tile + put_at(id, 0) + i * kPer * tile_ld<T, NX> : tile + put_at(id, i), v[i]);
   }
 };
 
 struct ChunkArgs {
-  View c, u, w, out;        // rows that multiply the state, its updates u w^T, results
-  View c2, out2;            // backwards: the rows v and results dk beside k and dv
+  // c: rows that multiply the state; u, w: its updates u w^T; out: results.
+  // Forwards c and out have G heads, backwards u and w.
+  View c, u, w, out;
   int G, na, nb, H, nseg;   // na rows and nb columns of the state
   int64_t T, L;             // tokens per segment, a multiple of kC
   float scale;
@@ -204,14 +269,21 @@ struct ChunkArgs {
   int sr, sc;               // element strides of the state's rows and columns
 };
 
+// One launch's work: dv and dk go together, each pair of workgroups eight
+// numbers apart, which the hardware gives to one XCD, so that the second finds
+// the rows of q and do that both read in its L2.
+struct Work {
+  ChunkArgs a[2];
+  int kinds, each;  // how many of a, and workgroups of each
+};
+
 struct Where {
   int b, h, seg;
   int64_t t0, t1, end;  // the segment's tokens t0 .. t1 - 1, of which those before `end` count
 };
 
-__device__ __forceinline__ Where where(const ChunkArgs& a) {
+__device__ __forceinline__ Where where(const ChunkArgs& a, int id) {
   Where x;
-  const int id = blockIdx.x;
   x.seg = id % a.nseg;
   x.h = id / a.nseg % a.H;
   x.b = id / a.nseg / a.H;
@@ -228,398 +300,285 @@ __device__ __forceinline__ T* at(const View& v, int b, int64_t t, int h) {
   return static_cast<T*>(v.p) + b * v.batch + t * v.step + h * v.head;
 }
 
-// Columns t0 .. of NT tiles of results, times f: eight (bf16) or four (fp32) per lane
-template <class T, int NT, int NO>
-__device__ __forceinline__ void store_row(T* row, int t0, const f4 (&o)[NO], float f, bool zero, int n) {
-  const int g = threadIdx.x % 64 / 16;
-#pragma unroll
-  for (int t = 0; t < NT; t += Mm<T>::kTiles) {
-    u4v v;
-    int col = 16 * (t0 + t);
-    if constexpr (sizeof(T) == 2) {
-      v = u4v{pk_bf16(o[t][0] * f, o[t][1] * f), pk_bf16(o[t][2] * f, o[t][3] * f), pk_bf16(o[t + 1][0] * f, o[t + 1][1] * f),
-              pk_bf16(o[t + 1][2] * f, o[t + 1][3] * f)};
-      col += 8 * g;
-    } else {
-      v = __builtin_bit_cast(u4v, f4{o[t][0] * f, o[t][1] * f, o[t][2] * f, o[t][3] * f});
-      col += 4 * g;
-    }
-    if (zero) v = u4v{0, 0, 0, 0};
-    if (col < n) *(u4u*)(row + col) = v;
+// four neighbouring results
+template <class T>
+__device__ __forceinline__ void store4(Global p, const f4& v) {
+  if constexpr (sizeof(T) == 2) {
+    typedef u2v __attribute__((aligned(2))) u2u;
+    *(__attribute__((address_space(1))) u2u*)p = u2v{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
+  } else {
+    typedef f4 __attribute__((aligned(4))) f4u;
+    *(__attribute__((address_space(1))) f4u*)p = v;
   }
 }
 
-// zeros for the results of tokens t .. t1 - 1
-template <class T, int NX>
-__device__ __forceinline__ void zero_rows(const View& out, int b, int h0, int heads, int64_t t, int64_t t1, int n) {
-  constexpr int lanes = NX * int(sizeof(T)) / 16;
-  const int col = threadIdx.x % lanes * (16 / int(sizeof(T)));
-  for (int64_t r = t + threadIdx.x / lanes; r < t1; r += kThreads / lanes)
-    if (col < n)
-      for (int g = 0; g < heads; ++g) *(u4u*)(at<T>(out, b, r, h0 + g) + col) = u4v{0, 0, 0, 0};
-}
-
-// The state of one segment in the accumulators of a workgroup's waves: wave w
-// holds the rows 16 MT (w % 4) .. and the tiles NT (w / 4) .. of columns.
-template <class T, int NA, int NB>
-struct State {
-  static constexpr int MT = NA / 64, NT = NB / 16 / kSets;
-  static constexpr int kLd = tile_ld<T, NA>, kPart = NB * kLd;  // of the copy in LDS
-  f4 s[MT][NT];
-
-  __device__ __forceinline__ int tile(int t) const { return threadIdx.x / 256 * NT + t; }
-  __device__ __forceinline__ int row_tile(int mt) const { return threadIdx.x / 64 % 4 * MT + mt; }
-  __device__ __forceinline__ int row(int mt) const { return row_tile(mt) * 16 + threadIdx.x % 64 / 16 * 4; }
-  __device__ __forceinline__ int column(int t) const { return Mm<T>::column(tile(t), threadIdx.x % 16); }
-
-  __device__ __forceinline__ void load(const float* p, const ChunkArgs& a) {
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          s[mt][t][r] = p && row(mt) + r < a.na && column(t) < a.nb ? p[(row(mt) + r) * a.sr + column(t) * a.sc] : 0.0f;
-  }
-  __device__ __forceinline__ void store(float* p, const ChunkArgs& a) const {
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (row(mt) + r < a.na && column(t) < a.nb) p[(row(mt) + r) * a.sr + column(t) * a.sc] = s[mt][t][r];
-  }
-  // the transposed copy that multiplies rows, in kHalves parts: line 16 t + n holds column(t, n)
-  __device__ __forceinline__ void put(char* lds) const {
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        Mm<T>::put4(lds + (16 * tile(t) + threadIdx.x % 16) * kLd + row(mt) * int(sizeof(T)), kPart, s[mt][t]);
-  }
-  // s = f s + sum over the chunk's rows of weight u w^T; weight(tile, r) is that of row 16 tile + 4 g + r
-  template <class Weight>
-  __device__ __forceinline__ void update(float f, const char* u, const char* w, Weight weight) {
-    constexpr int lu = tile_ld<T, NA>, lw = tile_ld<T, NB>, tiles = Mm<T>::kTiles, units = kC / (16 * tiles);
-    const int l = threadIdx.x % 64;
-    typename Mm<T>::Frag a[MT][units][Mm<T>::kParts];
-#pragma unroll
-    for (int i = 0; i < units; ++i) {
-      float by[4 * tiles];
-#pragma unroll
-      for (int k = 0; k < 4 * tiles; ++k) by[k] = weight(tiles * i + k / 4, k % 4);
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        const char* p = Mm<T>::token_lane(u, lu, l) + Mm<T>::token_plain_col(row_tile(mt), l);
-        Mm<T>::split(Mm<T>::token(p, lu, i), by, a[mt][i]);
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      typename Mm<T>::Frag b[units];
-#pragma unroll
-      for (int i = 0; i < units; ++i) b[i] = Mm<T>::token(Mm<T>::token_lane(w, lw, l) + Mm<T>::token_col(tile(t), l), lw, i);
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        f4 sum = {0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < units; ++i)
-#pragma unroll
-          for (int p = Mm<T>::kParts - 1; p >= 0; --p) sum = Mm<T>::mul(a[mt][i][p], b[i], sum);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[mt][t][r] = fmaf(f, s[mt][t][r], sum[r]);
-      }
-    }
-  }
+// A chunk's factors, behind the tiles in LDS.
+struct Tables {
+  float power[kC];   // of a row's products: scale lambda^n, n tokens apart
+  float weight[kC];  // of the rows of the update: lambda^(m-1-j); backwards scale lambda^(j+1)
+  float from[kC];    // of the state in a row's result: scale lambda^(i+1); backwards lambda^(m-1-j)
 };
 
-// acc[t] = f times lines 16 (t0 + t) .. of the state's copy times a row's fragments
-template <class T, int NA, int NB, int NT, int NO, int NC>
-__device__ __forceinline__ void times_state(f4 (&acc)[NO], int t0, const char* copy, const RowFrags<T, NC>& c, float f) {
-  constexpr int ld = State<T, NA, NB>::kLd, part = State<T, NA, NB>::kPart, units = RowFrags<T, NA>::kUnits;
-  const char* p = copy + (16 * t0 + threadIdx.x % 16) * ld + threadIdx.x % 64 / 16 * 16;
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    typename Mm<T>::Frag a[Mm<T>::kHalves][units];
-#pragma unroll
-    for (int h = 0; h < Mm<T>::kHalves; ++h)
-#pragma unroll
-      for (int u = 0; u < units; ++u) a[h][u] = *(const typename Mm<T>::Frag*)(p + h * part + 16 * t * ld + 64 * u);
-    f4 v = {0, 0, 0, 0};
-#pragma unroll
-    for (int h = Mm<T>::kHalves - 1; h >= 0; --h)
-#pragma unroll
-      for (int u = 0; u < units; ++u) v = Mm<T>::mul(a[h][u], c.f[u], v);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) acc[t][r] = v[r] * f;
-  }
-}
-
-// acc[t] = f times columns of the state's copy's lines (rows of the state) times a row's fragments
-template <class T, int NA, int NB, int NO, int NC>
-__device__ __forceinline__ void times_state_back(f4 (&acc)[NO], const char* copy, const RowFrags<T, NC>& c, float f) {
-  constexpr int ld = State<T, NA, NB>::kLd, part = State<T, NA, NB>::kPart, units = RowFrags<T, NB>::kUnits;
-  const int l = threadIdx.x % 64;
-  const char* p = Mm<T>::token_lane(copy, ld, l);
-#pragma unroll
-  for (int t = 0; t < NA / 16; ++t) {
-    typename Mm<T>::Frag a[Mm<T>::kHalves][units];
-#pragma unroll
-    for (int h = 0; h < Mm<T>::kHalves; ++h)
-#pragma unroll
-      for (int u = 0; u < units; ++u) a[h][u] = Mm<T>::token(p + h * part + Mm<T>::token_col(t, l), ld, u);
-    f4 v = {0, 0, 0, 0};
-#pragma unroll
-    for (int h = Mm<T>::kHalves - 1; h >= 0; --h)
-#pragma unroll
-      for (int u = 0; u < units; ++u) v = Mm<T>::mul(a[h][u], c.f[u], v);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) acc[t][r] = v[r] * f;
-  }
-}
-
-// the products of 16 rows of a tile in LDS with a row's fragments: row 4 g + r in p[r]
-template <class T, int NX, int NC>
-__device__ __forceinline__ f4 dots(const char* tile, int jt, const RowFrags<T, NC>& c) {
-  constexpr int ld = tile_ld<T, NX>, units = RowFrags<T, NX>::kUnits;
-  const char* p = tile + (16 * jt + threadIdx.x % 16) * ld + threadIdx.x % 64 / 16 * 16;
-  typename Mm<T>::Frag a[units];
-  f4 v = {0, 0, 0, 0};
-#pragma unroll
-  for (int u = 0; u < units; ++u) a[u] = *(const typename Mm<T>::Frag*)(p + 64 * u);
-#pragma unroll
-  for (int u = 0; u < units; ++u) v = Mm<T>::mul(a[u], c.f[u], v);
-  return v;
-}
-
-// acc[t] += tiles t0 + t of a transposed tile of 64 rows times weighted products
-template <class T, int NX, int NT, int NO>
-__device__ __forceinline__ void times_tile(f4 (&acc)[NO], int t0, const char* tile, int unit,
-                                           const typename Mm<T>::Frag (&p)[Mm<T>::kHalves]) {
-  constexpr int ld = tile_ld<T, NX>;
-  const int l = threadIdx.x % 64;
-  const char* q = Mm<T>::token_lane(tile, ld, l);
-  typename Mm<T>::Frag a[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) a[t] = Mm<T>::token(q + Mm<T>::token_col(t0 + t, l), ld, unit);
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int h = Mm<T>::kHalves - 1; h >= 0; --h) acc[t] = Mm<T>::mul(a[t], p[h], acc[t]);
-}
-
 template <class T, int NA, int NB>
-constexpr int chunk_lds() {
-  return kC * (tile_ld<T, NA> + tile_ld<T, NB>)+Mm<T>::kHalves * State<T, NA, NB>::kPart;
-}
+struct Plan {
+  static constexpr int kWaves = NB / 16, kThreads = 64 * kWaves;
+  static constexpr int kUnits = kRows / Mm<T>::kTiles;                    // token units of a chunk
+  static constexpr int kTileA = kC * tile_ld<T, NA>, kTileB = kC * tile_ld<T, NB>;
+  static constexpr int kDots = kRows * kUnits * Mm<T>::kHalves * 1024;    // the exchanged products
+  static constexpr int kLds = 2 * kTileA + kTileB + kDots + int(sizeof(Tables));
+};
 
-// Forwards: results of a segment's tokens (OUT), or the state that the segment
-// alone leaves.
-template <class T, int NA, int NB, bool OUT>
-__global__ __launch_bounds__(kThreads, 2) void forwards(ChunkArgs a) {
-  extern __shared__ __align__(16) char lds[];
-  constexpr int units = kC / (16 * Mm<T>::kTiles), NT = NB / 16 / kSets;
-  char* const ut = lds;
-  char* const wt = ut + kC * tile_ld<T, NA>;
-  char* const copy = wt + kC * tile_ld<T, NB>;
-  const Where x = where(a);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) % 4, n = threadIdx.x % 16, g = threadIdx.x % 64 / 16;
-  const float ld = a.log_decay[x.h];
-  const int64_t state = (int64_t(x.b) * a.H + x.h) * a.nseg + x.seg;
-
-  State<T, NA, NB> S;
-  S.load(OUT && a.s0 ? a.s0 + state * a.na * a.nb : nullptr, a);
-  const float whole = power(ld, kC);
-  // lambda^(i-j) for this lane's row i = 16 wave + n and j = 16 jt + 4 g + r:
-  // far[wave - jt] near[r] below the diagonal tile, both with exponents >= 0
-  float diag[4], near[4], far[4], after[4];
+// S = whole S + the columns of u's tile in LDS times the rows w, each with its
+// weight: the parts FIRST .. LAST - 1 of those
+template <class T, int NA, int FIRST, int LAST, int AHEAD>
+__device__ __forceinline__ void update(f4 (&S)[NA / 16], float whole, typename Mm<T>::Frag (&w)[kRows / Mm<T>::kTiles],
+                                       unsigned u, unsigned state_at, const float* weight) {
+  typedef Mm<T> M;
+  constexpr int units = kRows / M::kTiles, ld = tile_ld<T, NA>;
+  const int g = here(threadIdx.x) % 64 / 16;
+  typename M::Frag b[units][LAST], f[AHEAD][units];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    diag[r] = n >= 4 * g + r ? power(ld, n - 4 * g - r) : 0.0f;
-    near[r] = power(ld, 15 - 4 * g - r);
-    far[r] = power(ld, r ? 16 * r + n - 15 : 0);
-    after[r] = power(ld, kC - 16 - 16 * r);
+  for (int i = 0; i < units; ++i) {
+    float by[4 * M::kTiles];
+#pragma unroll
+    for (int k = 0; k < M::kTiles; ++k) {
+      const f4 v = *(const f4*)(weight + 16 * (M::kTiles * i + k) + 4 * g);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) by[4 * k + r] = v[r];
+    }
+    M::split(w[i], by, b[i]);
   }
-  const float own = power(ld, 16 * wave + n + 1);
-
-  Stage<T, NA> su;
-  Stage<T, NB> sw;
-  RowFrags<T, NA> c, next;
-  const int i = 16 * wave + n;
-  auto fetch = [&](int64_t t) {
-    const int m = int(min(int64_t(kC), x.end - t));
-    su.load(at<T>(a.u, x.b, t, x.h), a.u.step, m, a.na);
-    sw.load(at<T>(a.w, x.b, t, x.h), a.w.step, m, a.nb);
+  auto columns = [&](int d) {
+    const unsigned at = M::state_tile(state_at, d);
+#pragma unroll
+    for (int i = 0; i < units; ++i) f[d % AHEAD][i] = M::token(at + u, ld, i);
   };
-  auto fetch_row = [&](int64_t t, int q) { next.load(at<T>(a.c, x.b, t + i, x.h * a.G + q), t + i < x.end, a.na); };
-  if (x.t0 < x.end) {
-    fetch(x.t0);
-    if (OUT) fetch_row(x.t0, 0);
-  }
-  int64_t t = x.t0;
-  for (; t < x.end; t += kC) {
-    const int m = int(min(int64_t(kC), x.end - t)), rows = int(min(int64_t(kC), x.t1 - t));
-    su.put(ut), sw.put(wt);
-    if (OUT) S.put(copy);
-    __syncthreads();
-    if (t + kC < x.end) fetch(t + kC);
-    if (OUT) {
-      for (int q = 0; q < a.G; ++q) {
-        c = next;
-        if (q + 1 < a.G)
-          fetch_row(t, q + 1);
-        else if (t + kC < x.end)
-          fetch_row(t + kC, 0);
-        f4 o[NT];
-        times_state<T, NA, NB, NT>(o, S.tile(0), copy, c, own);
+  if (AHEAD > 1) columns(0);
 #pragma unroll
-        for (int u = 0; u < units; ++u) {
-          if (u * Mm<T>::kTiles > wave) continue;
-          f4 p[Mm<T>::kTiles];
+  for (int d = 0; d < NA / 16; ++d) {
+    if (AHEAD == 1 || d + 1 < NA / 16) columns(AHEAD == 1 ? d : d + 1);  // two: on their way during this tile's products
+    f4 sum = {0, 0, 0, 0};
 #pragma unroll
-          for (int k = 0; k < Mm<T>::kTiles; ++k) {
-            const int jt = u * Mm<T>::kTiles + k;
-            p[k] = f4{0, 0, 0, 0};
-            if (jt > wave) continue;
-            const f4 v = dots<T, NA>(ut, jt, c);
-            const float f = wave - jt == 1 ? far[1] : wave - jt == 2 ? far[2] : far[3];
+    for (int i = 0; i < units; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-              p[k][r] = jt == wave ? (n >= 4 * g + r ? v[r] * diag[r] : 0.0f) : v[r] * (f * near[r]);
-          }
-          typename Mm<T>::Frag pf[Mm<T>::kHalves];
-          Mm<T>::pack(p, pf);
-          times_tile<T, NB, NT>(o, S.tile(0), wt, u, pf);
-        }
-        if (i < rows) store_row<T, NT>(at<T>(a.out, x.b, t + i, x.h * a.G + q), S.tile(0), o, a.scale, i >= m, a.nb);
-      }
-    }
-    if (m == kC)
-      S.update(whole, ut, wt, [&](int tile, int r) { return after[tile] * near[r]; });
-    else
-      S.update(power(ld, m), ut, wt, [&](int tile, int r) { return power(ld, max(0, m - 1 - 16 * tile - 4 * g - r)); });
-    __syncthreads();
-  }
-  if (OUT) zero_rows<T, NB>(a.out, x.b, x.h * a.G, a.G, t, x.t1, a.nb);
-  if (a.sn) S.store(a.sn + state * a.na * a.nb, a);
-}
-
-// One side of a chunk's gradients: o = (scale lambda^(i-j) (rows i of `left` . c))
-// summed over the rows of `right`, the rows i >= j of this lane's row j.
-template <class T, int NL, int NR, int NO, int NC>
-__device__ __forceinline__ void later_rows(f4 (&o)[NO], const char* left, const char* right, const RowFrags<T, NC>& c,
-                                           int wave, const float (&diag)[4], const float (&near)[4], const float (&far)[4]) {
-  constexpr int units = kC / (16 * Mm<T>::kTiles);
-  const int n = threadIdx.x % 16, g = threadIdx.x % 64 / 16;
+      for (int p = LAST - 1; p >= FIRST; --p) sum = M::mul(f[d % AHEAD][i], b[i][p], sum);
 #pragma unroll
-  for (int u = 0; u < units; ++u) {
-    if (u * Mm<T>::kTiles + Mm<T>::kTiles - 1 < wave) continue;
-    f4 p[Mm<T>::kTiles];
-#pragma unroll
-    for (int k = 0; k < Mm<T>::kTiles; ++k) {
-      const int it = u * Mm<T>::kTiles + k;
-      p[k] = f4{0, 0, 0, 0};
-      if (it < wave) continue;
-      const f4 v = dots<T, NL>(left, it, c);
-      const float f = it - wave == 1 ? far[1] : it - wave == 2 ? far[2] : far[3];
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        p[k][r] = it == wave ? (4 * g + r >= n ? v[r] * diag[r] : 0.0f) : v[r] * (f * near[r]);
-    }
-    typename Mm<T>::Frag pf[Mm<T>::kHalves];
-    Mm<T>::pack(p, pf);
-    times_tile<T, NR, NR / 16>(o, 0, right, u, pf);
+    for (int r = 0; r < 4; ++r) S[d][r] = fmaf(whole, S[d][r], sum[r]);
   }
 }
 
-// Backwards: u = q and w = do of G heads, c = k, c2 = v; out = dv, out2 = dk
-// (OUT), or the gradient that the segment alone leaves at its start.  The first
-// four waves form dv and the others dk.
-template <class T, int NA, int NB, bool OUT>
-__global__ __launch_bounds__(kThreads, 2) void backwards(ChunkArgs a) {
-  extern __shared__ __align__(16) char lds[];
-  constexpr int NX = NA > NB ? NA : NB;
-  char* const ut = lds;
-  char* const wt = ut + kC * tile_ld<T, NA>;
-  char* const copy = wt + kC * tile_ld<T, NB>;
-  const Where x = where(a);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) % 4, n = threadIdx.x % 16, g = threadIdx.x % 64 / 16;
-  const bool first = __builtin_amdgcn_readfirstlane(threadIdx.x / 256) == 0;
+// Results of a segment's tokens (OUT), or the state that the segment alone
+// leaves.  BACK: from the last token to the first.  EXACT: the last state is a
+// result (sn).  ONE: the group has one head (what passes from head to head
+// takes no registers).
+template <class T, int NA, int NB, bool BACK, bool OUT, bool EXACT, bool ONE>
+__global__ __launch_bounds__(64 * (NB / 16), sizeof(T) == 2 ? 4 : 2) void chunks(Work job) {
+  typedef Mm<T> M;
+  typedef Plan<T, NA, NB> P;
+  typedef typename M::Frag Frag;
+  extern __shared__ __align__(1024) char lds[];
+  constexpr unsigned ct = 0, ut = P::kTileA, wt = 2 * P::kTileA, pt = wt + P::kTileB;
+  Tables* const tab = reinterpret_cast<Tables*>(lds + pt + P::kDots);
+  constexpr int lda = tile_ld<T, NA>, ldb = tile_ld<T, NB>, TA = NA / 16, units = P::kUnits;
+  // fragments of LDS rows at a time: two of them take registers that the
+  // backward kernels of the full size do not have
+  constexpr int AHEAD = BACK && NA == 128 && sizeof(T) == 2 ? 1 : 2;
+
+  const int id = job.kinds == 1 ? blockIdx.x : blockIdx.x / 16 * 8 + blockIdx.x % 8;
+  if (id >= job.each) return;
+  const ChunkArgs a = job.a[job.kinds == 1 ? 0 : blockIdx.x / 8 % 2];
+  const Where x = where(a, id);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, n = lane % 16, g = lane / 16;
   const float ld = a.log_decay[x.h];
-  const int64_t state = (int64_t(x.b) * a.H + x.h) * a.nseg + x.seg;
+  const int64_t state = ((int64_t(x.b) * a.H + x.h) * a.nseg + x.seg) * a.na * a.nb;
+  const int col = 16 * wave + n;  // this lane's column of the state
 
-  State<T, NA, NB> D;
-  D.load(OUT && a.s0 ? a.s0 + state * a.na * a.nb : nullptr, a);
-  // lambda^(i-j) scale for this lane's row j = 16 wave + n and i = 16 it + 4 g + r
-  float diag[4], near[4], far[4], after[4];
+  f4 S[TA];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    diag[r] = 4 * g + r >= n ? a.scale * power(ld, 4 * g + r - n) : 0.0f;
-    near[r] = a.scale * power(ld, 4 * g + r);
-    far[r] = power(ld, r ? 16 * r - n : 0);
-    after[r] = power(ld, 16 * r + 1);
-  }
+  for (int t = 0; t < TA; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      S[t][r] = OUT && a.s0 && M::row(t, r) < a.na && col < a.nb ? a.s0[state + M::row(t, r) * a.sr + col * a.sc] : 0.0f;
+  if (threadIdx.x < kC) tab->power[threadIdx.x] = a.scale * power(ld, threadIdx.x);
 
-  Stage<T, NA> su;
-  Stage<T, NB> sw;
-  RowFrags<T, NX> c, next;
-  const int j = 16 * wave + n;
+  // this lane's addresses in LDS: row fragments, columns of the state's rows
+  // and of its own columns, pieces on their way there, exchanged products
+  const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds;
+  const unsigned row_at = base + tile_at<T, NA>(n, 16 * g), state_at = M::template state_at<NA>();
+  Stage<T, NA, P::kThreads> sc, su;
+  Stage<T, NB, P::kThreads> sw;
   auto fetch = [&](int64_t t, int q) {
     const int m = int(min(int64_t(kC), x.end - t));
-    su.load(at<T>(a.u, x.b, t, x.h * a.G + q), a.u.step, m, a.na);
-    sw.load(at<T>(a.w, x.b, t, x.h * a.G + q), a.w.step, m, a.nb);
+    if (OUT && (!BACK || q == 0)) sc.load(at<T>(a.c, x.b, t, BACK ? x.h : x.h * a.G + q), a.c.step, m, a.na);
+    if (BACK || q == 0) {
+      su.load(at<T>(a.u, x.b, t, BACK ? x.h * a.G + q : x.h), a.u.step, m, a.na);
+      sw.load(at<T>(a.w, x.b, t, BACK ? x.h * a.G + q : x.h), a.w.step, m, a.nb);
+    }
   };
-  auto fetch_rows = [&](int64_t t) {
-    next.load(first ? at<T>(a.c, x.b, t + j, x.h) : at<T>(a.c2, x.b, t + j, x.h), t + j < x.end, first ? a.na : a.nb);
-  };
-  const int64_t past = x.t0 + (max(x.end - x.t0, int64_t(0)) + kC - 1) / kC * kC;
-  if (past > x.t0) {
-    fetch(past - kC, 0);
-    if (OUT) fetch_rows(past - kC);
-  }
-  for (int64_t t = past - kC; t >= x.t0; t -= kC) {
-    const int m = int(min(int64_t(kC), x.end - t)), rows = int(min(int64_t(kC), x.t1 - t));
-    f4 o[NX / 16];
-    for (int q = 0; q < a.G; ++q) {
-      su.put(ut), sw.put(wt);
-      if (OUT && q == 0) D.put(copy);
+
+  const int heads = !ONE && (OUT || BACK) ? a.G : 1;
+  const int count = int((max(x.end - x.t0, int64_t(0)) + kC - 1) / kC);
+  if (count) fetch(x.t0 + (BACK ? count - 1 : 0) * int64_t(kC), 0);
+  const float full = power(ld, kC);
+  for (int k = 0, last = kC, m; k < count; ++k, last = m) {
+    const int64_t t = x.t0 + (BACK ? count - 1 - k : k) * int64_t(kC);
+    m = int(min(int64_t(kC), x.end - t));
+    f4 o[kRows];
+    for (int q = 0; q < heads; ++q) {
+      if (OUT && (!BACK || q == 0)) sc.to(base + ct);
+      if (BACK || q == 0) su.to(base + ut), sw.to(base + wt);
+      if (q == 0 && (k == 0 || m < kC || last < kC) && threadIdx.x < kC) {  // they are a whole chunk's otherwise
+        const int j = here(threadIdx.x), left = max(m - 1 - j, 0);
+        tab->weight[j] = BACK ? a.scale * power(ld, j + 1) : power(ld, left);
+        tab->from[j] = BACK ? power(ld, left) : a.scale * power(ld, j + 1);
+      }
       __syncthreads();
-      if (OUT && q == 0) c = next;
-      if (q + 1 < a.G) {
+      if (q + 1 < heads)
         fetch(t, q + 1);
-      } else if (t > x.t0) {
-        fetch(t - kC, 0);
-        if (OUT) fetch_rows(t - kC);
-      }
+      else if (k + 1 < count)
+        fetch(t + (BACK ? -kC : kC), 0);
+
       if (OUT) {
-        if (q == 0) {
-          const float own = power(ld, max(0, m - 1 - j));
-          if (first)
-            times_state<T, NA, NB, NB / 16>(o, 0, copy, c, own);
-          else
-            times_state_back<T, NA, NB>(o, copy, c, own);
+        // the weighted products of c's rows 16 it .. with u's rows of a unit
+        for (int item = wave; item < kRows * units; item += P::kWaves) {
+          const int it = item % kRows, unit = item / kRows;
+          if (BACK ? M::kTiles * unit + M::kTiles - 1 < it : M::kTiles * unit > it) continue;
+          f4 p[M::kTiles] = {};
+#pragma unroll
+          for (int d0 = 0; d0 < NA * int(sizeof(T)) / 64; d0 += 2) {
+            Frag cf[2], uf[M::kTiles][2];
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+              const unsigned at = flip(row_at, 64 * (d0 + d));
+              cf[d] = get<Frag>(at + ct + 16 * it * lda);
+#pragma unroll
+              for (int i = 0; i < M::kTiles; ++i) uf[i][d] = get<Frag>(at + ut + 16 * (M::kTiles * unit + i) * lda);
+            }
+#pragma unroll
+            for (int d = 0; d < 2; ++d)
+#pragma unroll
+              for (int i = 0; i < M::kTiles; ++i) p[i] = M::mul(uf[i][d], cf[d], p[i]);
+          }
+#pragma unroll
+          for (int i = 0; i < M::kTiles; ++i) {
+            const int jt = M::kTiles * unit + i;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int far = BACK ? 16 * (jt - it) + 4 * g + r - n : 16 * (it - jt) + n - 4 * g - r;
+              p[i][r] = far >= 0 ? p[i][r] * tab->power[max(far, 0)] : 0.0f;
+            }
+          }
+          Frag f[M::kHalves];
+          M::pack(p, f);
+          const unsigned dot_at = base + pt + here(threadIdx.x) % 64 * 16;
+#pragma unroll
+          for (int h = 0; h < M::kHalves; ++h) put(dot_at + ((it * units + unit) * M::kHalves + h) * 1024, f[h]);
         }
-        if (first)
-          later_rows<T, NA, NB>(o, ut, wt, c, wave, diag, near, far);
-        else
-          later_rows<T, NB, NA>(o, wt, ut, c, wave, diag, near, far);
+        // the state times c's rows
+        if (!BACK || q == 0) {
+#pragma unroll
+          for (int it = 0; it < kRows; ++it) o[it] = f4{0, 0, 0, 0};
+          Frag c[AHEAD][kRows];
+          auto rows = [&](int d) {
+            const unsigned at = flip(row_at, 64 * d);
+#pragma unroll
+            for (int it = 0; it < kRows; ++it) c[d % AHEAD][it] = get<Frag>(at + ct + 16 * it * lda);
+          };
+          if (AHEAD > 1) rows(0);
+#pragma unroll
+          for (int d = 0; d < TA / M::kTiles; ++d) {
+            if (AHEAD == 1 || d + 1 < TA / M::kTiles) rows(AHEAD == 1 ? d : d + 1);  // two: on their way during this unit's products
+            f4 s[M::kTiles];
+#pragma unroll
+            for (int i = 0; i < M::kTiles; ++i) s[i] = S[M::kTiles * d + i];
+            Frag f[M::kHalves];
+            M::pack(s, f);
+#pragma unroll
+            for (int h = M::kHalves - 1; h >= 0; --h)
+#pragma unroll
+              for (int it = 0; it < kRows; ++it) o[it] = M::mul(f[h], c[d % AHEAD][it], o[it]);
+          }
+#pragma unroll
+          for (int it = 0; it < kRows; ++it) {
+            const float f = tab->from[16 * it + n];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[it][r] *= f;
+          }
+        }
+        __syncthreads();
       }
-      D.update(q ? 1.0f : power(ld, m), ut, wt, [&](int tile, int r) { return after[tile] * near[r]; });
+
+      Frag w[units];
+      const unsigned own_at = base + wt + M::template token_at<NB>(here(threadIdx.x) % 64, wave);
+#pragma unroll
+      for (int u = 0; u < units; ++u) w[u] = M::token(own_at, ldb, u);
+      if (OUT) {
+        const unsigned dot_at = base + pt + here(threadIdx.x) % 64 * 16;
+#pragma unroll
+        for (int u = 0; u < units; ++u) {
+#pragma unroll
+          for (int h = M::kHalves - 1; h >= 0; --h) {
+            Frag p[kRows];
+#pragma unroll
+            for (int it = 0; it < kRows; ++it)
+              if (BACK ? M::kTiles * u + M::kTiles - 1 >= it : M::kTiles * u <= it)
+                p[it] = get<Frag>(dot_at + ((it * units + u) * M::kHalves + h) * 1024);
+#pragma unroll
+            for (int it = 0; it < kRows; ++it)
+              if (BACK ? M::kTiles * u + M::kTiles - 1 >= it : M::kTiles * u <= it) o[it] = M::mul(w[u], p[it], o[it]);
+          }
+        }
+        // The next rows are in registers by now.  Waited for here, before the
+        // stores, which the same counter counts, they need no wait that would
+        // take the stores' time too.
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+        if ((!BACK || q + 1 == heads) && 16 * wave < a.nb) {
+          char* const p = reinterpret_cast<char*>(at<T>(a.out, x.b, t, BACK ? x.h : x.h * a.G + q));
+          const int64_t tile = 16 * a.out.step * int64_t(sizeof(T));
+          const unsigned l = here(threadIdx.x) % 64;
+          const unsigned own = (l % 16 * unsigned(a.out.step) + 16 * wave + l / 16 * 4) * unsigned(sizeof(T));
+          if (m == kC) {
+#pragma unroll
+            for (int it = 0; it < kRows; ++it) store4<T>(shared_here(p + it * tile) + own, o[it]);
+          } else {  // the rows past the last token are zeros, those past the segment another's
+            const int rows = int(min(int64_t(kC), x.t1 - t));
+#pragma unroll
+            for (int it = 0; it < kRows; ++it) {
+              const int i = 16 * it + n;
+              if (i < rows) store4<T>(shared_here(p + it * tile) + own, i < m ? o[it] : f4{0, 0, 0, 0});
+            }
+          }
+        }
+      }
+      if (BACK || q + 1 == heads) {
+        // S = lambda^m S + sum of u (weight w)^T
+        const float whole = BACK && q ? 1.0f : m == kC ? full : power(ld, m);
+        if constexpr (EXACT && BACK && OUT && M::kParts == 3) {
+          // in two goes: the fragments of all three parts at once would push
+          // the rows on their way out of the registers
+          update<T, NA, 2, 3, AHEAD>(S, whole, w, base + ut, state_at, tab->weight);
+          update<T, NA, 0, 2, AHEAD>(S, 1.0f, w, base + ut, state_at, tab->weight);
+        } else {
+          update<T, NA, 0, EXACT || M::kParts == 1 ? M::kParts : 2, AHEAD>(S, whole, w, base + ut, state_at, tab->weight);
+        }
+      }
       __syncthreads();
     }
-    if (OUT && j < rows) {
-      if (first)
-        store_row<T, NB / 16>(at<T>(a.out, x.b, t + j, x.h), 0, o, 1.0f, j >= m, a.nb);
-      else
-        store_row<T, NA / 16>(at<T>(a.out2, x.b, t + j, x.h), 0, o, 1.0f, j >= m, a.na);
-    }
   }
-  if (OUT) {
-    zero_rows<T, NB>(a.out, x.b, x.h, 1, past, x.t1, a.nb);
-    zero_rows<T, NA>(a.out2, x.b, x.h, 1, past, x.t1, a.na);
+  if (OUT) {  // zeros for the tokens past the row's length
+    const int heads = BACK ? 1 : a.G;
+    for (int64_t t = x.t0 + int64_t(count) * kC + n; t < x.t1; t += 16)
+      if (16 * wave < a.nb)
+        for (int q = 0; q < heads; ++q)
+          store4<T>((Global)(uint64_t)(at<T>(a.out, x.b, t, x.h * heads + q) + 16 * wave + 4 * g), f4{0, 0, 0, 0});
   }
-  if (a.sn) D.store(a.sn + state * a.na * a.nb, a);
+  if (EXACT && a.sn) {
+#pragma unroll
+    for (int t = 0; t < TA; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (M::row(t, r) < a.na && col < a.nb) a.sn[state + M::row(t, r) * a.sr + col * a.sc] = S[t][r];
+  }
 }
 
 // Passes the states from segment to segment: what each segment alone leaves,
@@ -656,30 +615,43 @@ __global__ __launch_bounds__(256) void pass_states(PassArgs a) {
   if (a.sn) a.sn[int64_t(bh) * a.size + i] = s;
 }
 
-template <class T, int NA, int NB, bool BACK, bool OUT>
-hipError_t run_chunks(const ChunkArgs& a, int B, hipStream_t s) {
-  constexpr int lds = chunk_lds<T, NA, NB>();
-  void (*const f)(ChunkArgs) = BACK ? backwards<T, NA, NB, OUT> : forwards<T, NA, NB, OUT>;
-  if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute((const void*)f, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+template <class T, int NA, int NB, bool BACK, bool OUT, bool EXACT, bool ONE>
+hipError_t run_form(const Work& job, hipStream_t s) {
+  typedef Plan<T, NA, NB> P;
+  void (*const f)(Work) = chunks<T, NA, NB, BACK, OUT, EXACT, ONE>;
+  if (P::kLds > 65536) {
+    const hipError_t e = hipFuncSetAttribute((const void*)f, hipFuncAttributeMaxDynamicSharedMemorySize, P::kLds);
     if (e != hipSuccess) return e;
   }
-  f<<<unsigned(B) * a.H * a.nseg, kThreads, lds, s>>>(a);
+  const unsigned grid = job.kinds == 1 ? job.each : (job.each + 7) / 8 * 16;
+  f<<<grid, P::kThreads, P::kLds, s>>>(job);
   return hipGetLastError();
 }
 
+template <class T, int NA, int NB, bool BACK, bool OUT>
+hipError_t run_chunks(const Work& job, hipStream_t s) {
+  // fp32 kernels have no form for states that are no result: they split nothing
+  constexpr bool split = OUT && Mm<T>::kParts > 1;
+  const bool one = OUT && job.a[0].G == 1;
+  if (split && !job.a[0].sn)
+    return one ? run_form<T, NA, NB, BACK, OUT, !split, OUT>(job, s) : run_form<T, NA, NB, BACK, OUT, !split, false>(job, s);
+  return one ? run_form<T, NA, NB, BACK, OUT, true, OUT>(job, s) : run_form<T, NA, NB, BACK, OUT, true, false>(job, s);
+}
+
+// `b`: a second kind of work for the same kernel, or NULL
 template <bool BACK, bool OUT>
-hipError_t launch_chunks(const ChunkArgs& a, int bf16, int B, hipStream_t s) {
+hipError_t launch_chunks(const ChunkArgs& a, const ChunkArgs* b, int bf16, int B, hipStream_t s) {
+  const Work job{{a, b ? *b : a}, b ? 2 : 1, B * a.H * a.nseg};
   const int form = (bf16 ? 4 : 0) + (a.na > 64 ? 2 : 0) + (a.nb > 64 ? 1 : 0);
   switch (form) {
-    case 0: return run_chunks<float, 64, 64, BACK, OUT>(a, B, s);
-    case 1: return run_chunks<float, 64, 128, BACK, OUT>(a, B, s);
-    case 2: return run_chunks<float, 128, 64, BACK, OUT>(a, B, s);
-    case 3: return run_chunks<float, 128, 128, BACK, OUT>(a, B, s);
-    case 4: return run_chunks<__bf16, 64, 64, BACK, OUT>(a, B, s);
-    case 5: return run_chunks<__bf16, 64, 128, BACK, OUT>(a, B, s);
-    case 6: return run_chunks<__bf16, 128, 64, BACK, OUT>(a, B, s);
-    default: return run_chunks<__bf16, 128, 128, BACK, OUT>(a, B, s);
+    case 0: return run_chunks<float, 64, 64, BACK, OUT>(job, s);
+    case 1: return run_chunks<float, 64, 128, BACK, OUT>(job, s);
+    case 2: return run_chunks<float, 128, 64, BACK, OUT>(job, s);
+    case 3: return run_chunks<float, 128, 128, BACK, OUT>(job, s);
+    case 4: return run_chunks<__bf16, 64, 64, BACK, OUT>(job, s);
+    case 5: return run_chunks<__bf16, 64, 128, BACK, OUT>(job, s);
+    case 6: return run_chunks<__bf16, 128, 64, BACK, OUT>(job, s);
+    default: return run_chunks<__bf16, 128, 128, BACK, OUT>(job, s);
   }
 }
 
@@ -726,7 +698,7 @@ hipError_t pass(const AttnArgs& a, const Cut& c, float* ws, const float* s0, flo
 hipError_t segment_states(const AttnArgs& a, const Cut& c, float* ws, float* sn, hipStream_t s) {
   ChunkArgs r = base(a, c);
   r.u = a.k, r.w = a.v, r.sn = ws;
-  TRY((launch_chunks<false, false>(r, a.bf16, a.B, s)));
+  TRY((launch_chunks<false, false>(r, nullptr, a.bf16, a.B, s)));
   return pass<false>(a, c, ws, a.s0, sn, s);
 }
 
@@ -746,29 +718,33 @@ hipError_t launch_attn(const AttnArgs& a, hipStream_t s) {
     TRY(segment_states(a, c, ws, a.sn, s));
     r.s0 = ws, r.sn = nullptr;
   }
-  return launch_chunks<false, true>(r, a.bf16, a.B, s);
+  return launch_chunks<false, true>(r, nullptr, a.bf16, a.B, s);
 }
 
 hipError_t launch_attn_backward(const AttnGradArgs& g, hipStream_t s) {
   const AttnArgs& a = g.a;
   const Cut c = cut(a);
-  ChunkArgs f = base(a, c), r = base(a, c);
-  // dq: forwards over the transposed states
-  f.c = a.o, f.u = a.v, f.w = a.k, f.out = g.dq, f.s0 = a.s0;
-  f.na = a.dv, f.nb = a.dk, f.sr = 1, f.sc = a.dv;
-  r.c = a.k, r.c2 = a.v, r.u = a.q, r.w = a.o, r.out = g.dv, r.out2 = g.dk, r.s0 = g.dsn, r.sn = g.ds0;
+  ChunkArgs dq = base(a, c), dv = base(a, c);
+  dq.c = a.o, dq.u = a.v, dq.w = a.k, dq.out = g.dq, dq.s0 = a.s0;
+  dq.na = a.dv, dq.nb = a.dk, dq.sr = 1, dq.sc = a.dv;  // the transposed states
+  dv.c = a.k, dv.u = a.q, dv.w = a.o, dv.out = g.dv, dv.s0 = g.dsn, dv.sn = g.ds0;
   if (c.nseg > 1) {
     float* ws = reinterpret_cast<float*>(a.ws);
     float* ws2 = reinterpret_cast<float*>(a.ws + states_bytes(a, c));
     TRY(segment_states(a, c, ws, nullptr, s));
-    ChunkArgs l = r;
-    l.sn = ws2;
-    TRY((launch_chunks<true, false>(l, a.bf16, a.B, s)));
+    ChunkArgs own = dv;
+    own.sn = ws2;
+    TRY((launch_chunks<true, false>(own, nullptr, a.bf16, a.B, s)));
     TRY(pass<true>(a, c, ws2, g.dsn, g.ds0, s));
-    f.s0 = ws, r.s0 = ws2, r.sn = nullptr;
+    dq.s0 = ws, dv.s0 = ws2, dv.sn = nullptr;
   }
-  TRY((launch_chunks<false, true>(f, a.bf16, a.B, s)));
-  return launch_chunks<true, true>(r, a.bf16, a.B, s);
+  ChunkArgs dk = dv;
+  dk.c = a.v, dk.u = a.o, dk.w = a.q, dk.out = g.dk, dk.sn = nullptr;
+  dk.na = a.dv, dk.nb = a.dk, dk.sr = 1, dk.sc = a.dv;
+  TRY((launch_chunks<false, true>(dq, nullptr, a.bf16, a.B, s)));
+  if ((a.dk > 64) == (a.dv > 64)) return launch_chunks<true, true>(dv, &dk, a.bf16, a.B, s);
+  TRY((launch_chunks<true, true>(dv, nullptr, a.bf16, a.B, s)));
+  return launch_chunks<true, true>(dk, nullptr, a.bf16, a.B, s);
 }
 
 }  // namespace ambptt

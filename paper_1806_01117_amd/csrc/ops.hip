@@ -42,6 +42,9 @@ ambptt_status check_view(const ambptt_attention* a, const ambptt_view* v, int he
   REFUSE(!v || (!v->p && a->steps > 0), AMBPTT_EINVAL, "an operand is NULL");
   REFUSE(misaligned(v->p, size_of(a->dtype)), AMBPTT_EINVAL, "an operand is not aligned to its elements");
   REFUSE(v->batch < 0 || v->step < 0 || v->head < 0, AMBPTT_EINVAL, "strides must be >= 0");
+  // the kernels reach 16 tokens from one address by 32-bit offsets
+  REFUSE(a->steps > 1 && v->step > (int64_t(1) << 28) / size_of(a->dtype), AMBPTT_EUNSUPPORTED,
+         "a token more than 2^28 bytes from the next");
   if (out) {
     REFUSE((a->batch > 1 && v->batch < size) || (a->steps > 1 && v->step < size) || (heads > 1 && v->head < size),
            AMBPTT_EINVAL, "an output's elements overlap");
