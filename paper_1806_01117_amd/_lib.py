@@ -140,7 +140,8 @@ def load():
     L.ambptt_run_noalloc.restype = C.c_int
     L.ambptt_destroy.argtypes = [vp]
     L.ambptt_destroy.restype = None
-    att, view, nrm, drop = C.POINTER(Attention), C.POINTER(View), C.POINTER(Norm), C.POINTER(Drop)
+    att, nrm, drop = C.POINTER(Attention), C.POINTER(Norm), C.POINTER(Drop)
+    view = vp  # View, or as many int64 that ops.py passes in its place
     L.ambptt_decay_attention_workspace.argtypes = [att, i32, C.POINTER(sz)]
     L.ambptt_decay_attention.argtypes = [att, view, view, view, vp, vp, vp, view, vp, vp, sz, vp]
     L.ambptt_decay_attention_backward.argtypes = [att, view, view, view, vp, vp, vp, view, vp, view, view, view, vp, vp,

@@ -1,0 +1,107 @@
+// Attention whose state decays, one token: S = lambda S + k v^T, o = scale S^T q.
+//
+// The state is read and written once and is nearly all that moves, so a
+// workgroup takes one state and each thread four neighbouring columns of every
+// so many rows, with up to eight rows on their way at a time.  The products with
+// the group's queries are summed over a thread's rows, and then over the
+// threads of a column in LDS, in a fixed order.
+#include "ops.hpp"
+
+namespace ambptt {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kAhead = 8;  // rows on their way
+constexpr int kMaxDk = 128;
+constexpr int kHeads = 4;  // query heads at a time
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+
+template <class T>
+__device__ __forceinline__ const T* row_of(const View& v, int b, int h) {
+  return static_cast<const T*>(v.p) + b * v.batch + h * v.head;
+}
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void step(AttnArgs a) {
+  __shared__ float ks[kMaxDk], qs[kHeads][kMaxDk];
+  __shared__ f4 part[kHeads][kThreads];
+  const int h = blockIdx.x % a.H, b = blockIdx.x / a.H, tid = threadIdx.x;
+  const int lanes = a.dv / 4, groups = kThreads / lanes, row = tid / lanes, col = tid % lanes * 4;
+  const bool has = row < groups;
+  const int64_t at = int64_t(blockIdx.x) * a.dk * a.dv;
+  const float* const s0 = a.s0 ? a.s0 + at : nullptr;
+  float* const sn = a.sn ? a.sn + at : nullptr;
+  const bool live = !a.lengths || a.lengths[b] > 0;
+  // lambda - 1: fp32 holds it to 24 bits where lambda itself, rounded, would be
+  // off by n 2^-25 after n steps
+  const float less = live ? expm1f(a.log_decay[h]) : 0.0f;
+
+  f4 v = {0, 0, 0, 0};
+  if (live && has) {
+    const T* p = row_of<T>(a.v, b, h) + col;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = float(p[i]);
+  }
+  if (tid < a.dk) ks[tid] = live ? float(row_of<T>(a.k, b, h)[tid]) : 0.0f;
+  // kHeads heads at a time: one group of them goes with the state's update, a
+  // larger group reads the new state (or without sn forms it) again
+  for (int q0 = 0; q0 < a.G; q0 += kHeads) {
+    const int heads = min(kHeads, a.G - q0);
+    for (int q = 0; q < kHeads; ++q)
+      if (tid < a.dk) qs[q][tid] = live && q < heads ? float(row_of<T>(a.q, b, h * a.G + q0 + q)[tid]) * a.scale : 0.0f;
+    __syncthreads();
+    f4 o[kHeads] = {};
+    if (has) {
+      const float* const from = q0 && sn ? sn : s0;
+      const bool update = q0 == 0 || !sn;
+      for (int d0 = row; d0 < a.dk; d0 += groups * kAhead) {
+        f4 s[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          const int d = d0 + i * groups;
+          s[i] = from && d < a.dk ? *(const f4*)(from + d * a.dv + col) : f4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          const int d = d0 + i * groups;
+          if (d >= a.dk) break;
+          if (update) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[i][c] += fmaf(s[i][c], less, ks[d] * v[c]);
+            if (q0 == 0 && sn && (live || sn != s0)) *(f4*)(sn + d * a.dv + col) = s[i];
+          }
+#pragma unroll
+          for (int q = 0; q < kHeads; ++q)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[q][c] = fmaf(qs[q][d], s[i][c], o[q][c]);
+        }
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < kHeads; ++q)
+      if (q < heads) part[q][tid] = o[q];
+    __syncthreads();
+    for (int i = tid; i < heads * a.dv; i += kThreads) {
+      const int q = i / a.dv, c = i % a.dv;
+      float sum = 0.0f;
+      if (live)
+        for (int g = 0; g < groups; ++g) sum += part[q][g * lanes + c / 4][c % 4];
+      static_cast<T*>(a.o.p)[b * a.o.batch + (h * a.G + q0 + q) * a.o.head + c] = T(sum);
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_attn_step(const AttnArgs& a, hipStream_t s) {
+  const unsigned grid = unsigned(a.B) * a.H;
+  if (a.bf16)
+    step<__bf16><<<grid, kThreads, 0, s>>>(a);
+  else
+    step<float><<<grid, kThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace ambptt

@@ -40,6 +40,7 @@ struct AttnGradArgs {
 
 size_t attn_workspace(const AttnArgs& a, bool backward);
 hipError_t launch_attn(const AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_step(const AttnArgs& a, hipStream_t s);  // T = 1
 hipError_t launch_attn_backward(const AttnGradArgs& a, hipStream_t s);
 
 struct DropArgs {

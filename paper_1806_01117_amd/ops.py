@@ -7,7 +7,9 @@ with the names of the result, as ``Runner.run`` takes it).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
+import functools
 
 from . import _lib
 from ._lib import load
@@ -28,26 +30,26 @@ def _check(status: int) -> None:
         _lib.check(status)
 
 
-class _On:
-    """The device of `t` as the current one (a no-op where it is already)."""
+@contextlib.contextmanager
+def _device(torch, index):
+    with torch.cuda.device(index):
+        yield
 
-    def __init__(self, t):
-        torch = _t()
-        if t.device.type != "cuda":
-            raise ValueError(f"want cuda tensors, got {t.device}")
-        self.guard = torch.cuda.device(t.device) if t.device.index != torch.cuda.current_device() else None
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
+_HERE = contextlib.nullcontext()
 
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+
+def _on(t):
+    """A context with t's device as the current one (nothing to do where it is already)."""
+    torch = _t()
+    if not t.is_cuda:
+        raise ValueError(f"want cuda tensors, got {t.device}")
+    index = t.get_device()
+    return _HERE if index == torch._C._cuda_getDevice() else _device(torch, index)
 
 
 def _stream(t) -> int:
-    return _t()._C._cuda_getCurrentRawStream(t.device.index)
+    return _t()._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _dtype(name, t) -> int:
@@ -61,7 +63,7 @@ def _dtype(name, t) -> int:
 
 def _like(name, t, shape, ref, dtype=None):
     """`t` has the shape, and `ref`'s dtype (or `dtype`) and device."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != (dtype or ref.dtype) or t.device != ref.device:
+    if t.shape != shape or t.dtype != (dtype or ref.dtype) or t.get_device() != ref.get_device():
         raise ValueError(f"{name}: want {ref.device} {dtype or ref.dtype} {tuple(shape)}, got "
                          f"{t.device} {t.dtype} {tuple(t.shape)}")
     return t
@@ -84,11 +86,19 @@ def _ptr(t):
 # ---- attention ----------------------------------------------------------------
 
 
-def _view(name, t):
-    b, s, h, i = t.stride()
-    if i != 1 and t.shape[3] > 1:
-        raise ValueError(f"{name}: the elements of a head must be contiguous")
-    return C.byref(_lib.View(t.data_ptr(), b, s, h))
+_Views4, _Views7 = C.c_int64 * 16, C.c_int64 * 28  # four and seven C views {pointer, batch, step, head}
+
+
+def _views(kind, *tensors):
+    """The C views of [batch, steps, heads, size] tensors, as the arguments of a call."""
+    flat = []
+    for t in tensors:
+        b, s, h, i = t.stride()
+        if i != 1 and t.shape[3] > 1:
+            raise ValueError(f"the elements of a head must be contiguous, got strides {tuple(t.stride())}")
+        flat += t.data_ptr(), b, s, h
+    a = kind(*flat)
+    return [C.byref(a, 32 * n) for n in range(len(tensors))]
 
 
 def _attention(q, k, v, log_decay, lengths, scale):
@@ -97,28 +107,44 @@ def _attention(q, k, v, log_decay, lengths, scale):
     if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
         raise ValueError("q, k and v: want [batch, steps, heads, size]")
     B, T, HQ, dk = q.shape
-    H, dv = k.shape[2], v.shape[3]
+    _, _, H, dv = v.shape
     if H < 1 or HQ % H:
         raise ValueError(f"{HQ} query heads do not share {H} key/value heads evenly")
-    _like("k", k, (B, T, H, dk), q)
-    _like("v", v, (B, T, H, dv), q)
+    dt, dev = q.dtype, q.get_device()
+    if k.shape != (B, T, H, dk) or v.shape != (B, T, H, dv) or k.dtype != dt or v.dtype != dt or \
+            k.get_device() != dev or v.get_device() != dev:
+        _like("k", k, (B, T, H, dk), q)
+        _like("v", v, (B, T, H, dv), q)
     _dense("log_decay", log_decay, (H,), q, torch.float32)
-    _dense("lengths", lengths, (B,), q, torch.int32)
-    return _lib.Attention(_dtype("q", q), B, H, HQ // H, dk, dv, T, dk ** -0.5 if scale is None else scale), \
-        (B, T, HQ, H, dk, dv)
+    if lengths is not None:
+        _dense("lengths", lengths, (B,), q, torch.int32)
+    sizes = _dtype("q", q), B, H, HQ // H, dk, dv, T
+    return _lib.Attention(*sizes, dk ** -0.5 if scale is None else scale), sizes, (B, T, HQ, H, dk, dv)
 
 
-def _workspace(call, arg, *more, device):
+@functools.lru_cache(maxsize=256)
+def _attention_bytes(backward, *sizes):
     n = C.c_size_t()
-    _check(call(C.byref(arg), *more, C.byref(n)))
-    return (_t().empty(n.value, dtype=_t().uint8, device=device) if n.value else None), n.value
+    _check(load().ambptt_decay_attention_workspace(C.byref(_lib.Attention(*sizes, 1.0)), backward, C.byref(n)))
+    return n.value
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_bytes(rows, cols):
+    n = C.c_size_t()
+    _check(load().ambptt_add_norm_backward_workspace(C.byref(_lib.Norm(0, 0, rows, cols, 0, 0.0)), C.byref(n)))
+    return n.value
+
+
+def _workspace(n, ref):
+    return ref.new_empty(n, dtype=_t().uint8) if n else None
 
 
 def _result(out, name, shape, ref, dtype=None):
     """out[name], checked, or a new tensor."""
     t = out.get(name) if out else None
     if t is None:
-        return _t().empty(shape, dtype=dtype or ref.dtype, device=ref.device)
+        return ref.new_empty(shape) if dtype is None else ref.new_empty(shape, dtype=dtype)
     return _like(name, t, shape, ref, dtype)
 
 
@@ -133,16 +159,19 @@ def decay_attention(q, k, v, log_decay, s0=None, lengths=None, scale=None, out: 
     after them.  out["sn"] may be s0.
     """
     torch = _t()
-    a, (B, T, HQ, H, dk, dv) = _attention(q, k, v, log_decay, lengths, scale)
-    with _On(q):
+    a, sizes, (B, T, HQ, H, dk, dv) = _attention(q, k, v, log_decay, lengths, scale)
+    with _on(q):
         state = (B, H, dk, dv)
         _dense("s0", s0, state, q, torch.float32)
         o = _result(out, "o", (B, T, HQ, dv), q)
-        sn = _dense("sn", _result(out, "sn", state, q, torch.float32), state, q, torch.float32)
+        sn = s0 if out and s0 is not None and out.get("sn") is s0 else \
+            _dense("sn", _result(out, "sn", state, q, torch.float32), state, q, torch.float32)
         L = load()
-        ws, n = _workspace(L.ambptt_decay_attention_workspace, a, 0, device=q.device)
-        _check(L.ambptt_decay_attention(C.byref(a), _view("q", q), _view("k", k), _view("v", v), _ptr(log_decay),
-                                        _ptr(s0), _ptr(lengths), _view("o", o), _ptr(sn), _ptr(ws), n, _stream(q)))
+        n = _attention_bytes(0, *sizes)
+        ws = _workspace(n, q)
+        vq, vk, vv, vo = _views(_Views4, q, k, v, o)
+        _check(L.ambptt_decay_attention(C.byref(a), vq, vk, vv, log_decay.data_ptr(), _ptr(s0), _ptr(lengths), vo,
+                                        sn.data_ptr(), _ptr(ws), n, _stream(q)))
     return {"o": o, "sn": sn}
 
 
@@ -168,8 +197,8 @@ def decay_attention_backward(q, k, v, log_decay, do, s0=None, dsn=None, lengths=
     where s0 or dsn was given (or out["ds0"]), else None.
     """
     torch = _t()
-    a, (B, T, HQ, H, dk, dv) = _attention(q, k, v, log_decay, lengths, scale)
-    with _On(q):
+    a, sizes, (B, T, HQ, H, dk, dv) = _attention(q, k, v, log_decay, lengths, scale)
+    with _on(q):
         state = (B, H, dk, dv)
         _dense("s0", s0, state, q, torch.float32)
         _dense("dsn", dsn, state, q, torch.float32)
@@ -179,10 +208,11 @@ def decay_attention_backward(q, k, v, log_decay, do, s0=None, dsn=None, lengths=
         if s0 is not None or dsn is not None or (out and out.get("ds0") is not None):
             res["ds0"] = _dense("ds0", _result(out, "ds0", state, q, torch.float32), state, q, torch.float32)
         L = load()
-        ws, n = _workspace(L.ambptt_decay_attention_workspace, a, 1, device=q.device)
+        n = _attention_bytes(1, *sizes)
+        ws = _workspace(n, q)
+        vq, vk, vv, vo, v1, v2, v3 = _views(_Views7, q, k, v, do, res["dq"], res["dk"], res["dv"])
         _check(L.ambptt_decay_attention_backward(
-            C.byref(a), _view("q", q), _view("k", k), _view("v", v), _ptr(log_decay), _ptr(s0), _ptr(lengths),
-            _view("do", do), _ptr(dsn), _view("dq", res["dq"]), _view("dk", res["dk"]), _view("dv", res["dv"]),
+            C.byref(a), vq, vk, vv, log_decay.data_ptr(), _ptr(s0), _ptr(lengths), vo, _ptr(dsn), v1, v2, v3,
             _ptr(res["ds0"]), _ptr(ws), n, _stream(q)))
     return res
 
@@ -232,7 +262,7 @@ def dropout(x, p, seed, offset=0, residual=None, out=None):
     """
     dt = _dtype("x", x)
     rows, cols = _sizes("x", x)
-    with _On(x):
+    with _on(x):
         if residual is not None:
             _like("residual", residual, x.shape, x)
         y = _result({"out": out}, "out", x.shape, x)
@@ -266,7 +296,7 @@ def add_norm(x, w, residual=None, eps=1e-6, p=0.0, seed=0, offset=0, out_dtype=N
     f8 = out_dtype == "f8"
     dt = _dtype("x", x)
     a = _lib.Norm(dt, _lib.F8 if f8 else dt, rows, cols, scale_block, eps)
-    with _On(x):
+    with _on(x):
         if residual is not None:
             _like("residual", residual, x.shape, x)
         _dense("w", w, (cols,), x, torch.float32)
@@ -292,7 +322,7 @@ def add_norm_backward(dy, h, w, dh=None, eps=1e-6, p=0.0, seed=0, offset=0, out:
     rows, cols = _sizes("h", h)
     dt = _dtype("h", h)
     a = _lib.Norm(dt, dt, rows, cols, 0, eps)
-    with _On(h):
+    with _on(h):
         _like("dy", dy, h.shape, h)
         if dh is not None:
             _like("dh", dh, h.shape, h)
@@ -302,7 +332,8 @@ def add_norm_backward(dy, h, w, dh=None, eps=1e-6, p=0.0, seed=0, offset=0, out:
         dx = _result(out, "dx", h.shape, h) if drop is not None else None
         dw = _dense("dw", _result(out, "dw", (cols,), h, torch.float32), (cols,), h, torch.float32)
         L = load()
-        ws, n = _workspace(L.ambptt_add_norm_backward_workspace, a, device=h.device)
+        n = _norm_bytes(rows, cols)
+        ws = _workspace(n, h)
         _check(L.ambptt_add_norm_backward(
             C.byref(a), drop, *_rows("dy", dy), *(_rows("dh", dh) if dh is not None else (None, 0)), *_rows("h", h),
             _ptr(w), *_rows("dresidual", dr), *(_rows("dx", dx) if dx is not None else (None, 0)), _ptr(dw), _ptr(ws),
