@@ -116,7 +116,7 @@ enum { AMBPTT_F8 = 2 };  /* y in 8 bits: OCP e4m3, y ~= scale * stored, scale = 
 typedef struct {
   int32_t dtype;        /* AMBPTT_F32 | AMBPTT_BF16: x, residual, h and the gradients */
   int32_t out;          /* y: dtype, or AMBPTT_F8 */
-  int64_t rows, cols;   /* rows >= 0, 1 <= cols < 2^31 */
+  int64_t rows, cols;   /* 0 <= rows < 2^31, 1 <= cols <= 2^30 */
   int32_t scale_block;  /* F8: columns per scale, 0 (one per row) or 128 */
   float eps;
 } ambptt_norm;

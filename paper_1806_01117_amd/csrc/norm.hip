@@ -6,7 +6,17 @@ namespace ambptt {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kV = 8;  // columns per thread and step: the elements of one counter
+constexpr int kV = 8;  // columns per lane and piece of a row: the elements of one counter
+
+typedef unsigned int u4v __attribute__((ext_vector_type(4)));
+typedef unsigned int u2v __attribute__((ext_vector_type(2)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+// at any element's address
+typedef u4v __attribute__((aligned(2))) u4u;
+typedef f4 __attribute__((aligned(4))) f4u;
+typedef u2v __attribute__((aligned(1))) u2u;
 
 // Philox-4x32-10: the 128 bits of counter n under a 64-bit key.
 __device__ __forceinline__ uint4 philox(uint64_t n, uint64_t key) {
@@ -32,64 +42,164 @@ __device__ __forceinline__ void drop8(float (&v)[kV], const DropArgs& d, uint64_
   }
 }
 
-// columns c .. c + 7 of row r as fp32; zeros past the row's end
-template <class T>
-__device__ __forceinline__ void load8(float (&v)[kV], const Rows& x, int64_t r, int64_t c, int64_t cols) {
-  const T* p = static_cast<const T*>(x.p) + r * x.ld + c;
+// columns c .. c + 7 of a row as fp32; zeros past the row's end
+__device__ __forceinline__ void load8(float (&v)[kV], const __bf16* row, int c, int cols) {
+  if (c + kV <= cols) {
+    const u4v u = *(const u4u*)(row + c);
 #pragma unroll
-  for (int i = 0; i < kV; ++i) v[i] = c + i < cols ? float(p[i]) : 0.0f;
+    for (int i = 0; i < kV / 2; ++i)
+      v[2 * i] = __builtin_bit_cast(float, u[i] << 16), v[2 * i + 1] = __builtin_bit_cast(float, u[i] & 0xffff0000u);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kV; ++i) v[i] = c + i < cols ? float(row[c + i]) : 0.0f;
+  }
+}
+__device__ __forceinline__ void load8(float (&v)[kV], const float* row, int c, int cols) {
+  if (c + kV <= cols) {
+    const f4 a = *(const f4u*)(row + c), b = *(const f4u*)(row + c + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < kV; ++i) v[i] = c + i < cols ? row[c + i] : 0.0f;
+  }
+}
+__device__ __forceinline__ void store8(const float (&v)[kV], __bf16* row, int c, int cols) {
+  if (c + kV <= cols) {
+    u4v u;
+#pragma unroll
+    for (int i = 0; i < kV / 2; ++i)
+      u[i] = __builtin_bit_cast(unsigned, __builtin_convertvector(f2{v[2 * i], v[2 * i + 1]}, bf16x2));
+    *(u4u*)(row + c) = u;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kV; ++i)
+      if (c + i < cols) row[c + i] = __bf16(v[i]);
+  }
+}
+__device__ __forceinline__ void store8(const float (&v)[kV], float* row, int c, int cols) {
+  if (c + kV <= cols) {
+    *(f4u*)(row + c) = f4{v[0], v[1], v[2], v[3]};
+    *(f4u*)(row + c + 4) = f4{v[4], v[5], v[6], v[7]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < kV; ++i)
+      if (c + i < cols) row[c + i] = v[i];
+  }
 }
 template <class T>
-__device__ __forceinline__ void store8(const float (&v)[kV], const Rows& x, int64_t r, int64_t c, int64_t cols) {
-  T* p = static_cast<T*>(x.p) + r * x.ld + c;
-#pragma unroll
-  for (int i = 0; i < kV; ++i)
-    if (c + i < cols) p[i] = T(v[i]);
+__device__ __forceinline__ T* row_of(const Rows& x, int64_t r) {
+  return static_cast<T*>(x.p) + r * x.ld;
 }
 
+// Dropout: eight columns per thread and turn.  `wide` pieces make a row; their
+// numbers are divided by it with a multiplication (mul, shift), and with wide 0
+// all is one row.  blockIdx.y takes `per` rows, so that numbers fit in 31 bits.
+struct Pieces {
+  unsigned wide, mul;
+  int shift;
+  int64_t per;
+};
+constexpr int kTurns = 2;  // pieces of a thread on their way at a time
+
 template <class T>
-__global__ __launch_bounds__(kThreads) void dropout(DropoutArgs a) {
-  const int64_t wide = (a.cols + kV - 1) / kV;
-  const int64_t c8 = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-  if (c8 >= wide) return;
-  for (int64_t r = blockIdx.y; r < a.rows; r += gridDim.y) {
-    float v[kV];
-    load8<T>(v, a.x, r, c8 * kV, a.cols);
-    if (a.d.at) drop8(v, a.d, a.d.offset + r * wide + c8);
-    if (a.r.p) {
-      float q[kV];
-      load8<T>(q, a.r, r, c8 * kV, a.cols);
+__global__ __launch_bounds__(kThreads) void dropout(DropoutArgs a, Pieces w) {
+  const int64_t r0 = blockIdx.y * w.per;
+  const int64_t many = w.wide ? min(w.per, a.rows - r0) * w.wide : (a.cols + kV - 1) / kV;
+  const int64_t stride = int64_t(gridDim.x) * kThreads;
+  for (int64_t i0 = int64_t(blockIdx.x) * kThreads + threadIdx.x; i0 < many; i0 += kTurns * stride) {
+    float v[kTurns][kV], q[kTurns][kV];
+    int64_t at[kTurns];  // columns from the row's start, in the row of the pointers below
+    T* y[kTurns];
+    int64_t n[kTurns];
+    int cols[kTurns];
 #pragma unroll
-      for (int i = 0; i < kV; ++i) v[i] += q[i];
+    for (int k = 0; k < kTurns; ++k) {
+      const int64_t i = i0 + k * stride;
+      n[k] = -1;
+      if (i >= many) continue;
+      int64_t r = 0, c = i;
+      if (w.wide) {
+        r = w.wide == 1 ? i : __umulhi(unsigned(i), w.mul) >> w.shift;
+        c = i - r * w.wide;
+        n[k] = (r0 + r) * w.wide + c;
+      } else {
+        n[k] = i;
+      }
+      at[k] = c * kV;
+      cols[k] = int(min(int64_t(kV), a.cols - at[k]));
+      load8(v[k], row_of<T>(a.x, r0 + r) + at[k], 0, cols[k]);
+      if (a.r.p) load8(q[k], row_of<T>(a.r, r0 + r) + at[k], 0, cols[k]);
+      y[k] = row_of<T>(a.y, r0 + r) + at[k];
     }
-    store8<T>(v, a.y, r, c8 * kV, a.cols);
+#pragma unroll
+    for (int k = 0; k < kTurns; ++k) {
+      if (n[k] < 0) continue;
+      if (a.d.at) drop8(v[k], a.d, a.d.offset + n[k]);
+      if (a.r.p) {
+#pragma unroll
+        for (int e = 0; e < kV; ++e) v[k][e] += q[k][e];
+      }
+      store8(v[k], y[k], 0, cols[k]);
+    }
   }
 }
 
-// the sum (or the maximum) over a workgroup, in every thread; a fixed order
-template <bool MAX>
-__device__ __forceinline__ float block_all(float v, float* lds) {
+// The norm's rows.  A row of up to THREADS * NV * 8 columns is read once and
+// stays in the registers of one wave (THREADS 64, four rows to a workgroup) or
+// of a workgroup, NV pieces of eight columns to a lane; longer rows (NV 0) are
+// read again for each pass over them by one workgroup.
+template <int THREADS>
+constexpr int kRowsPer = THREADS == 64 ? 4 : 1;
+template <int THREADS>
+constexpr int kBlock = THREADS * kRowsPer<THREADS>;
+
+// the sum (or the maximum) over a row's threads, in each of them; a fixed order
+template <int THREADS, bool MAX>
+__device__ __forceinline__ float row_all(float v, float* lds) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) {
     const float u = __shfl_xor(v, o);
     v = MAX ? fmaxf(v, u) : v + u;
   }
-  __syncthreads();  // the last call's values are read
-  if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
-  __syncthreads();
-  v = lds[0];
+  if constexpr (THREADS > 64) {
+    __syncthreads();  // the last call's values are read
+    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
+    __syncthreads();
+    v = lds[0];
 #pragma unroll
-  for (int i = 1; i < kThreads / 64; ++i) v = MAX ? fmaxf(v, lds[i]) : v + lds[i];
+    for (int i = 1; i < THREADS / 64; ++i) v = MAX ? fmaxf(v, lds[i]) : v + lds[i];
+  }
   return v;
 }
+// two sums at once
+template <int THREADS>
+__device__ __forceinline__ void row_sums(float& v, float& u, float* lds) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o), u += __shfl_xor(u, o);
+  if constexpr (THREADS > 64) {
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v, lds[THREADS / 64 + threadIdx.x / 64] = u;
+    __syncthreads();
+    v = lds[0], u = lds[THREADS / 64];
+#pragma unroll
+    for (int i = 1; i < THREADS / 64; ++i) v += lds[i], u += lds[THREADS / 64 + i];
+  }
+}
 
+// h of columns c .. c + 7
 template <class T>
-__device__ __forceinline__ void load_h(float (&v)[kV], const NormArgs& a, int64_t r, int64_t c, int64_t wide) {
-  load8<T>(v, a.x, r, c, a.cols);
+__device__ __forceinline__ void load_h(float (&v)[kV], const NormArgs& a, int64_t r, int c, int64_t wide) {
+  if (c >= a.cols) {
+#pragma unroll
+    for (int i = 0; i < kV; ++i) v[i] = 0.0f;
+    return;
+  }
+  float q[kV];
+  load8(v, row_of<const T>(a.x, r), c, a.cols);
+  if (a.r.p) load8(q, row_of<const T>(a.r, r), c, a.cols);
   if (a.d.at) drop8(v, a.d, a.d.offset + r * wide + c / kV);
   if (a.r.p) {
-    float q[kV];
-    load8<T>(q, a.r, r, c, a.cols);
 #pragma unroll
     for (int i = 0; i < kV; ++i) v[i] += q[i];
   }
@@ -100,161 +210,333 @@ __device__ __forceinline__ uint32_t f8x2(float a, float b) {
   return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false)) & 0xffffu;
 }
 
-// One workgroup per row, which is read again for each pass over it (h may be
-// x or the residual, so it is stored in the last).
-template <class T>
-__global__ __launch_bounds__(kThreads) void add_norm(NormArgs a) {
-  __shared__ float lds[kThreads / 64];
-  const int64_t wide = (a.cols + kV - 1) / kV;
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    float sum = 0.0f;
-    for (int64_t c = threadIdx.x * kV; c < a.cols; c += kThreads * kV) {
-      float v[kV];
-      load_h<T>(v, a, r, c, wide);
+// y = w (h rr) of columns c .. c + 7
+__device__ __forceinline__ void times_w(float (&y)[kV], const float (&h)[kV], float rr, const NormArgs& a, int c) {
+  float w[kV];
+  load8(w, a.w, c, a.cols);
 #pragma unroll
-      for (int i = 0; i < kV; ++i) sum += v[i] * v[i];
+  for (int i = 0; i < kV; ++i) y[i] = w[i] * (h[i] * rr);
+}
+__device__ __forceinline__ float most_of(const float (&y)[kV]) {
+  float m = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kV; ++i) m = fmaxf(m, fabsf(y[i]));
+  return m;
+}
+
+// stores h and y of columns c .. c + 7; every lane of the row comes here (16 of
+// them share a block's maximum); `most` is the row's
+template <class T, bool F8>
+__device__ __forceinline__ void store_y(const float (&h)[kV], float (&y)[kV], float most, const NormArgs& a, int64_t r, int c) {
+  if (a.h.p && c < a.cols) store8(h, row_of<T>(a.h, r), c, a.cols);
+  if constexpr (!F8) {
+    if (c < a.cols) store8(y, row_of<T>(a.y, r), c, a.cols);
+  } else {
+    if (a.block) {
+      most = most_of(y);
+#pragma unroll
+      for (int o = 8; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
     }
-    const float rr = rsqrtf(block_all<false>(sum, lds) / float(a.cols) + a.eps);
-    float most = 0.0f;
-    if (a.f8 && !a.block) {
-      for (int64_t c = threadIdx.x * kV; c < a.cols; c += kThreads * kV) {
-        float v[kV];
-        load_h<T>(v, a, r, c, wide);
+    if (c >= a.cols) return;
+    const float scale = most > 0.0f ? most / 448.0f : 1.0f;
+    if (a.block ? c % 128 == 0 : c == 0) a.scale[a.block ? r * ((a.cols + 127) / 128) + c / 128 : r] = scale;
+    uint32_t u[kV / 2];
 #pragma unroll
-        for (int i = 0; i < kV; ++i)
-          if (c + i < a.cols) most = fmaxf(most, fabsf(a.w[c + i] * (v[i] * rr)));
-      }
-      most = block_all<true>(most, lds);
-    }
-    // every thread goes through the same steps: 16 lanes share a block's maximum
-    for (int64_t c0 = 0; c0 < a.cols; c0 += kThreads * kV) {
-      const int64_t c = c0 + threadIdx.x * kV;
-      float v[kV], y[kV];
-      load_h<T>(v, a, r, c, wide);
+    for (int i = 0; i < kV / 2; ++i) u[i] = f8x2(y[2 * i] / scale, y[2 * i + 1] / scale);
+    uint8_t* const p = row_of<uint8_t>(a.y, r) + c;
+    if (c + kV <= a.cols) {
+      *(u2u*)p = u2v{u[0] | u[1] << 16, u[2] | u[3] << 16};
+    } else {
 #pragma unroll
-      for (int i = 0; i < kV; ++i) y[i] = c + i < a.cols ? a.w[c + i] * (v[i] * rr) : 0.0f;
-      if (a.h.p) store8<T>(v, a.h, r, c, a.cols);
-      if (!a.f8) {
-        store8<T>(y, a.y, r, c, a.cols);
-        continue;
-      }
-      float top = most;
-      if (a.block) {
-        top = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kV; ++i) top = fmaxf(top, fabsf(y[i]));
-#pragma unroll
-        for (int o = 8; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-      }
-      const float scale = top > 0.0f ? top / 448.0f : 1.0f;
-      if (c < a.cols) {
-        if (a.block ? threadIdx.x % 16 == 0 : c == 0)
-          a.scale[a.block ? r * ((a.cols + 127) / 128) + c / 128 : r] = scale;
-        uint8_t* p = static_cast<uint8_t*>(a.y.p) + r * a.y.ld + c;
-#pragma unroll
-        for (int i = 0; i < kV; i += 2) {
-          const uint32_t u = f8x2(y[i] / scale, y[i + 1] / scale);
-          if (c + i < a.cols) p[i] = u & 0xff;
-          if (c + i + 1 < a.cols) p[i + 1] = u >> 8;
-        }
-      }
+      for (int i = 0; i < kV; ++i)
+        if (c + i < a.cols) p[i] = uint8_t(u[i / 2] >> 8 * (i % 2));
     }
   }
 }
 
-// Rows blockIdx.x, blockIdx.x + gridDim.x, ...: their dr, dx, and their sum of
-// dy h r in the workgroup's row of parts.
-template <class T>
-__global__ __launch_bounds__(kThreads) void add_norm_backward(NormGradArgs a) {
-  __shared__ float lds[kThreads / 64];
-  const int64_t wide = (a.cols + kV - 1) / kV;
+template <class T, int THREADS, int NV, bool F8>
+__global__ __launch_bounds__(kBlock<THREADS>) void add_norm(NormArgs a) {
+  __shared__ float lds[THREADS / 64 + 1];
+  const int64_t wide = (a.cols + kV - 1) / kV, rows = kRowsPer<THREADS>;
+  const int lane = threadIdx.x % THREADS;
   const float inv = 1.0f / float(a.cols);
-  bool first = true;
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, first = false) {
-    float hh = 0.0f, ah = 0.0f;
-    for (int64_t c = threadIdx.x * kV; c < a.cols; c += kThreads * kV) {
-      float h[kV], dy[kV];
-      load8<T>(h, a.h, r, c, a.cols);
-      load8<T>(dy, a.dy, r, c, a.cols);
+  for (int64_t r = blockIdx.x * rows + threadIdx.x / THREADS; r < a.rows; r += gridDim.x * rows) {
+    if constexpr (NV > 0) {
+      float h[NV][kV], sum = 0.0f;
 #pragma unroll
-      for (int i = 0; i < kV; ++i)
-        if (c + i < a.cols) hh += h[i] * h[i], ah += a.w[c + i] * dy[i] * h[i];
-    }
-    hh = block_all<false>(hh, lds), ah = block_all<false>(ah, lds);
-    const float rr = rsqrtf(hh * inv + a.eps), m = rr * rr * (ah * inv);
-    for (int64_t c = threadIdx.x * kV; c < a.cols; c += kThreads * kV) {
-      float h[kV], dy[kV], dr[kV];
-      load8<T>(h, a.h, r, c, a.cols);
-      load8<T>(dy, a.dy, r, c, a.cols);
-      if (a.dh.p) {
-        load8<T>(dr, a.dh, r, c, a.cols);
-      } else {
+      for (int k = 0; k < NV; ++k) load_h<T>(h[k], a, r, (k * THREADS + lane) * kV, wide);
 #pragma unroll
-        for (int i = 0; i < kV; ++i) dr[i] = 0.0f;
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int i = 0; i < kV; ++i) sum += h[k][i] * h[k][i];
+      const float rr = rsqrtf(row_all<THREADS, false>(sum, lds) * inv + a.eps);
+      float y[NV][kV], most = 0.0f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        times_w(y[k], h[k], rr, a, (k * THREADS + lane) * kV);
+        if (F8) most = fmaxf(most, most_of(y[k]));
       }
+      if (F8 && !a.block) most = row_all<THREADS, true>(most, lds);
 #pragma unroll
-      for (int i = 0; i < kV; ++i)
-        if (c + i < a.cols) {
-          dr[i] += rr * (a.w[c + i] * dy[i] - h[i] * m);
-          if (a.dw) {
-            float* p = a.parts + int64_t(blockIdx.x) * a.cols + c + i;
-            *p = (first ? 0.0f : *p) + dy[i] * (h[i] * rr);
-          }
+      for (int k = 0; k < NV; ++k) store_y<T, F8>(h[k], y[k], most, a, r, (k * THREADS + lane) * kV);
+    } else {
+      float sum = 0.0f, most = 0.0f, h[kV], y[kV];
+      for (int c = lane * kV; c < a.cols; c += THREADS * kV) {
+        load_h<T>(h, a, r, c, wide);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) sum += h[i] * h[i];
+      }
+      const float rr = rsqrtf(row_all<THREADS, false>(sum, lds) * inv + a.eps);
+      if (F8 && !a.block) {
+        for (int c = lane * kV; c < a.cols; c += THREADS * kV) {
+          load_h<T>(h, a, r, c, wide);
+          times_w(y, h, rr, a, c);
+          most = fmaxf(most, most_of(y));
         }
-      store8<T>(dr, a.dr, r, c, a.cols);
-      if (a.dx.p) {
-        if (a.d.at) drop8(dr, a.d, a.d.offset + r * wide + c / kV);
-        store8<T>(dr, a.dx, r, c, a.cols);
+        most = row_all<THREADS, true>(most, lds);
+      }
+      for (int c0 = 0; c0 < a.cols; c0 += THREADS * kV) {
+        const int c = c0 + lane * kV;
+        load_h<T>(h, a, r, c, wide);
+        times_w(y, h, rr, a, c);
+        store_y<T, F8>(h, y, most, a, r, c);  // h may be x or the residual: this piece is not read again
       }
     }
   }
 }
 
-// dw = the sum of `parts` rows, in order
+// dr (and dx) of columns c .. c + 7 from dr = dh
+template <class T>
+__device__ __forceinline__ void store_dr(float (&dr)[kV], const NormGradArgs& a, int64_t r, int c, int64_t wide) {
+  store8(dr, row_of<T>(a.dr, r), c, a.cols);
+  if (!a.dx.p) return;
+  if (a.d.at) drop8(dr, a.d, a.d.offset + r * wide + c / kV);
+  store8(dr, row_of<T>(a.dx, r), c, a.cols);
+}
+__device__ __forceinline__ void zero8(float (&v)[kV]) {
+#pragma unroll
+  for (int i = 0; i < kV; ++i) v[i] = 0.0f;
+}
+
+// Every gridDim.x-th group of rows: their dr, dx, and the sum of dy h r over
+// them in the workgroup's row of parts.
+template <class T, int THREADS, int NV>
+__global__ __launch_bounds__(kBlock<THREADS>) void add_norm_backward(NormGradArgs a) {
+  __shared__ float lds[2 * (THREADS / 64)];
+  extern __shared__ float sums[];  // THREADS 64: the waves' sums
+  const int64_t wide = (a.cols + kV - 1) / kV, rows = kRowsPer<THREADS>;
+  const int lane = threadIdx.x % THREADS, row = threadIdx.x / THREADS;
+  const float inv = 1.0f / float(a.cols);
+  float* const part = a.parts + int64_t(blockIdx.x) * a.cols;
+  if constexpr (NV > 0) {
+    float w[NV][kV], dw[NV][kV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (k * THREADS + lane) * kV;
+      zero8(dw[k]), zero8(w[k]);
+      if (c < a.cols) load8(w[k], a.w, c, a.cols);
+    }
+    for (int64_t r = blockIdx.x * rows + row; r < a.rows; r += gridDim.x * rows) {
+      float h[NV][kV], dy[NV][kV], dr[NV][kV], hh = 0.0f, ah = 0.0f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = (k * THREADS + lane) * kV;
+        zero8(h[k]), zero8(dy[k]), zero8(dr[k]);
+        if (c >= a.cols) continue;
+        load8(h[k], row_of<const T>(a.h, r), c, a.cols);
+        load8(dy[k], row_of<const T>(a.dy, r), c, a.cols);
+        if (a.dh.p) load8(dr[k], row_of<const T>(a.dh, r), c, a.cols);
+      }
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int i = 0; i < kV; ++i) hh += h[k][i] * h[k][i], ah += w[k][i] * dy[k][i] * h[k][i];
+      row_sums<THREADS>(hh, ah, lds);
+      const float rr = rsqrtf(hh * inv + a.eps), m = rr * rr * (ah * inv);
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = (k * THREADS + lane) * kV;
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+          dr[k][i] += rr * (w[k][i] * dy[k][i] - h[k][i] * m);
+          dw[k][i] += dy[k][i] * (h[k][i] * rr);
+        }
+        if (c < a.cols) store_dr<T>(dr[k], a, r, c, wide);
+      }
+    }
+    if (!a.dw) return;
+    if constexpr (THREADS == 64) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = (k * THREADS + lane) * kV;
+        if (c < a.cols) store8(dw[k], sums + row * a.cols, c, a.cols);
+      }
+      __syncthreads();
+      for (int c = threadIdx.x; c < a.cols; c += kBlock<THREADS>) {
+        float v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kRowsPer<THREADS>; ++k) v += sums[k * a.cols + c];
+        part[c] = v;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = (k * THREADS + lane) * kV;
+        if (c < a.cols) store8(dw[k], part, c, a.cols);
+      }
+    }
+  } else {
+    bool first = true;
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, first = false) {
+      float h[kV], dy[kV], dr[kV], w[kV], hh = 0.0f, ah = 0.0f;
+      for (int c = lane * kV; c < a.cols; c += THREADS * kV) {
+        load8(h, row_of<const T>(a.h, r), c, a.cols);
+        load8(dy, row_of<const T>(a.dy, r), c, a.cols);
+        load8(w, a.w, c, a.cols);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) hh += h[i] * h[i], ah += w[i] * dy[i] * h[i];
+      }
+      row_sums<THREADS>(hh, ah, lds);
+      const float rr = rsqrtf(hh * inv + a.eps), m = rr * rr * (ah * inv);
+      for (int c = lane * kV; c < a.cols; c += THREADS * kV) {
+        float sum[kV];
+        load8(h, row_of<const T>(a.h, r), c, a.cols);
+        load8(dy, row_of<const T>(a.dy, r), c, a.cols);
+        load8(w, a.w, c, a.cols);
+        zero8(dr), zero8(sum);
+        if (a.dh.p) load8(dr, row_of<const T>(a.dh, r), c, a.cols);
+        if (a.dw && !first) load8(sum, part, c, a.cols);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+          dr[i] += rr * (w[i] * dy[i] - h[i] * m);
+          sum[i] += dy[i] * (h[i] * rr);
+        }
+        if (a.dw) store8(sum, part, c, a.cols);
+        store_dr<T>(dr, a, r, c, wide);
+      }
+    }
+  }
+}
+
+// dw = the sum of `parts` rows: 32 columns to a workgroup, every eighth row to a
+// thread, then those eight, in a fixed order
 __global__ __launch_bounds__(kThreads) void sum_parts(const float* p, int parts, int cols, float* out) {
-  const int64_t c = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-  if (c >= cols) return;
+  __shared__ float lds[8][32];
+  const int c = blockIdx.x * 32 + threadIdx.x % 32, k = threadIdx.x / 32;
   float v = 0.0f;
-  for (int i = 0; i < parts; ++i) v += p[int64_t(i) * cols + c];
+  if (c < cols) {
+#pragma unroll 8
+    for (int i = k; i < parts; i += 8) v += p[int64_t(i) * cols + c];
+  }
+  lds[k][threadIdx.x % 32] = v;
+  __syncthreads();
+  if (k || c >= cols) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) v += lds[i][threadIdx.x];
   out[c] = v;
 }
 
-unsigned blocks(int64_t n, int64_t most) { return unsigned(n < 1 ? 1 : n < most ? n : most); }
+// Threads to a row and pieces to a lane.  One wave takes rows of up to 1024
+// columns, and of 2048 where there are enough of them to fill the CUs with
+// waves of their own; then a workgroup.
+struct Form {
+  int threads, nv;
+};
+Form form_of(int64_t rows, int64_t cols) {
+  if (cols <= 512) return {64, 1};
+  if (cols <= 1024) return {64, 2};
+  if (cols <= 2048) return rows >= 4096 ? Form{64, 4} : Form{256, 1};
+  if (cols <= 4096) return {256, 2};
+  if (cols <= 8192) return {256, 4};
+  if (cols <= 16384) return {1024, 2};
+  return {1024, 0};
+}
+
+template <class T, int THREADS, int NV>
+hipError_t run_norm(const NormArgs& a, hipStream_t s) {
+  const int64_t groups = (a.rows + kRowsPer<THREADS> - 1) / kRowsPer<THREADS>, grid = groups < 65536 ? groups : 65536;
+  if (a.f8)
+    add_norm<T, THREADS, NV, true><<<unsigned(grid), kBlock<THREADS>, 0, s>>>(a);
+  else
+    add_norm<T, THREADS, NV, false><<<unsigned(grid), kBlock<THREADS>, 0, s>>>(a);
+  return hipGetLastError();
+}
+template <class T, int THREADS, int NV>
+hipError_t run_norm_backward(const NormGradArgs& a, hipStream_t s) {
+  const unsigned grid = unsigned(norm_grad_parts(a.rows, a.cols)), lds = THREADS == 64 ? 4 * a.cols * 4 : 0;
+  add_norm_backward<T, THREADS, NV><<<grid, kBlock<THREADS>, lds, s>>>(a);
+  return hipGetLastError();
+}
+
+#define BY_FORM(run, T, a, s)                                 \
+  switch (form_of(a.rows, a.cols).threads * 8 + form_of(a.rows, a.cols).nv) { \
+    case 64 * 8 + 1: return run<T, 64, 1>(a, s);              \
+    case 64 * 8 + 2: return run<T, 64, 2>(a, s);              \
+    case 64 * 8 + 4: return run<T, 64, 4>(a, s);              \
+    case 256 * 8 + 1: return run<T, 256, 1>(a, s);            \
+    case 256 * 8 + 2: return run<T, 256, 2>(a, s);            \
+    case 256 * 8 + 4: return run<T, 256, 4>(a, s);            \
+    case 1024 * 8 + 2: return run<T, 1024, 2>(a, s);          \
+    default: return run<T, 1024, 0>(a, s);                    \
+  }
+
+template <class T>
+hipError_t norm_by_form(const NormArgs& a, hipStream_t s) {
+  BY_FORM(run_norm, T, a, s)
+}
+template <class T>
+hipError_t norm_backward_by_form(const NormGradArgs& a, hipStream_t s) {
+  BY_FORM(run_norm_backward, T, a, s)
+}
 
 }  // namespace
 
-hipError_t launch_dropout(const DropoutArgs& a, hipStream_t s) {
-  const int64_t wide = (a.cols + kV - 1) / kV;
-  const dim3 grid(unsigned((wide + kThreads - 1) / kThreads), blocks(a.rows, 65535));
+hipError_t launch_dropout(const DropoutArgs& in, hipStream_t s) {
+  DropoutArgs a = in;
+  const bool dense = a.cols % kV == 0 && (a.rows == 1 || (a.x.ld == a.cols && a.y.ld == a.cols && (!a.r.p || a.r.ld == a.cols)));
+  Pieces w{};
+  int64_t many, slices = 1;
+  if (dense) {  // one row: pieces need no division, and their counters are the rows' counters in order
+    a.cols *= a.rows, a.rows = 1;
+    many = a.cols / kV;
+  } else {
+    w.wide = unsigned((a.cols + kV - 1) / kV);
+    int bits = 0;
+    while ((uint64_t(1) << bits) < w.wide) ++bits;
+    // n / wide = (n mul) >> (31 + bits) for n below 2^31: mul = ceil(2^(31 + bits) / wide)
+    if (bits) w.mul = unsigned(((uint64_t(1) << (31 + bits)) + w.wide - 1) / w.wide), w.shift = bits - 1;
+    w.per = (int64_t(1) << 31) / w.wide;
+    if (w.per > a.rows) w.per = a.rows;
+    slices = (a.rows + w.per - 1) / w.per;
+    many = w.per * w.wide;
+  }
+  const int64_t blocks = (many + kThreads * kTurns - 1) / (kThreads * kTurns);
+  const dim3 grid(unsigned(blocks < 8192 ? blocks : 8192), unsigned(slices));
   if (a.bf16)
-    dropout<__bf16><<<grid, kThreads, 0, s>>>(a);
+    dropout<__bf16><<<grid, kThreads, 0, s>>>(a, w);
   else
-    dropout<float><<<grid, kThreads, 0, s>>>(a);
+    dropout<float><<<grid, kThreads, 0, s>>>(a, w);
   return hipGetLastError();
 }
 
 hipError_t launch_add_norm(const NormArgs& a, hipStream_t s) {
-  const unsigned grid = blocks(a.rows, 65535);
-  if (a.bf16)
-    add_norm<__bf16><<<grid, kThreads, 0, s>>>(a);
-  else
-    add_norm<float><<<grid, kThreads, 0, s>>>(a);
-  return hipGetLastError();
+  return a.bf16 ? norm_by_form<__bf16>(a, s) : norm_by_form<float>(a, s);
 }
 
-int norm_grad_parts(int64_t rows, int64_t) { return int(blocks(rows, 512)); }
+// as many workgroups as the CUs hold at once, and no more than there are rows for
+int norm_grad_parts(int64_t rows, int64_t cols) {
+  const Form f = form_of(rows, cols);
+  const int64_t groups = f.threads == 64 ? (rows + 3) / 4 : rows, most = f.threads == 1024 ? 512 : 1024;
+  return int(groups < 1 ? 1 : groups < most ? groups : most);
+}
 
 hipError_t launch_add_norm_backward(const NormGradArgs& a, hipStream_t s) {
-  const unsigned parts = unsigned(norm_grad_parts(a.rows, a.cols));
   if (a.rows) {
-    if (a.bf16)
-      add_norm_backward<__bf16><<<parts, kThreads, 0, s>>>(a);
-    else
-      add_norm_backward<float><<<parts, kThreads, 0, s>>>(a);
-    if (const hipError_t e = hipGetLastError()) return e;
+    const hipError_t e = a.bf16 ? norm_backward_by_form<__bf16>(a, s) : norm_backward_by_form<float>(a, s);
+    if (e != hipSuccess) return e;
   }
   if (!a.dw) return hipSuccess;
-  sum_parts<<<unsigned((a.cols + kThreads - 1) / kThreads), kThreads, 0, s>>>(a.parts, a.rows ? int(parts) : 0, a.cols, a.dw);
+  sum_parts<<<unsigned((a.cols + 31) / 32), kThreads, 0, s>>>(a.parts, a.rows ? norm_grad_parts(a.rows, a.cols) : 0, a.cols, a.dw);
   return hipGetLastError();
 }
 

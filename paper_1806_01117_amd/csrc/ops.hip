@@ -32,8 +32,9 @@ ambptt_status check_attention(const ambptt_attention* a) {
   REFUSE(a->dk % 16 || a->dv % 16 || a->dk > 128 || a->dv > 128, AMBPTT_EUNSUPPORTED,
          "head sizes must be multiples of 16 from 16 to 128");
   REFUSE(a->steps > INT32_MAX, AMBPTT_EUNSUPPORTED, "steps must be below 2^31");
-  REFUSE((int64_t)a->batch * a->heads > (int64_t(1) << 24) || (int64_t)a->heads * a->group > (int64_t(1) << 24),
-         AMBPTT_EUNSUPPORTED, "more than 2^24 states or query heads");
+  // a grid has fewer than 2^32 threads
+  REFUSE((int64_t)a->batch * a->heads > (int64_t(1) << 21) || (int64_t)a->heads * a->group > (int64_t(1) << 24),
+         AMBPTT_EUNSUPPORTED, "more than 2^21 states or 2^24 query heads");
   return AMBPTT_OK;
 }
 
@@ -88,7 +89,7 @@ ambptt_status check_norm(const ambptt_norm* n) {
   REFUSE(!size_of(n->dtype), AMBPTT_EINVAL, "unknown dtype");
   REFUSE(n->rows < 0 || n->cols < 1, AMBPTT_EINVAL, "need rows >= 0 and cols >= 1");
   REFUSE(!(n->eps >= 0.0f) || !std::isfinite(n->eps), AMBPTT_EINVAL, "eps must be finite and >= 0");
-  REFUSE(n->cols > INT32_MAX, AMBPTT_EUNSUPPORTED, "cols must be below 2^31");
+  REFUSE(n->cols > (int64_t(1) << 30) || n->rows > INT32_MAX, AMBPTT_EUNSUPPORTED, "more than 2^30 columns or 2^31 - 1 rows");
   return AMBPTT_OK;
 }
 
