@@ -320,8 +320,12 @@ __device__ __forceinline__ void zero8(float (&v)[kV]) {
 
 // Every gridDim.x-th group of rows: their dr, dx, and the sum of dy h r over
 // them in the workgroup's row of parts.
+// (waves per SIMD of the backward kernel: what norm_grad_parts counts on)
+template <int THREADS, int NV>
+constexpr int kWavesBack = THREADS == 1024 || NV < 4 ? 4 : 2;
+
 template <class T, int THREADS, int NV>
-__global__ __launch_bounds__(kBlock<THREADS>) void add_norm_backward(NormGradArgs a) {
+__global__ __launch_bounds__(kBlock<THREADS>, (kWavesBack<THREADS, NV>)) void add_norm_backward(NormGradArgs a) {
   __shared__ float lds[2 * (THREADS / 64)];
   extern __shared__ float sums[];  // THREADS 64: the waves' sums
   const int64_t wide = (a.cols + kV - 1) / kV, rows = kRowsPer<THREADS>;
@@ -526,7 +530,7 @@ hipError_t launch_add_norm(const NormArgs& a, hipStream_t s) {
 // as many workgroups as the CUs hold at once, and no more than there are rows for
 int norm_grad_parts(int64_t rows, int64_t cols) {
   const Form f = form_of(rows, cols);
-  const int64_t groups = f.threads == 64 ? (rows + 3) / 4 : rows, most = f.threads == 1024 ? 512 : 1024;
+  const int64_t groups = f.threads == 64 ? (rows + 3) / 4 : rows, most = f.threads == 1024 ? 256 : f.nv == 4 ? 512 : 1024;
   return int(groups < 1 ? 1 : groups < most ? groups : most);
 }
 

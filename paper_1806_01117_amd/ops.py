@@ -63,6 +63,8 @@ def _dtype(name, t) -> int:
 
 def _like(name, t, shape, ref, dtype=None):
     """`t` has the shape, and `ref`'s dtype (or `dtype`) and device."""
+    if t is None:
+        raise ValueError(f"{name} is required")
     if t.shape != shape or t.dtype != (dtype or ref.dtype) or t.get_device() != ref.get_device():
         raise ValueError(f"{name}: want {ref.device} {dtype or ref.dtype} {tuple(shape)}, got "
                          f"{t.device} {t.dtype} {tuple(t.shape)}")
@@ -222,7 +224,10 @@ def decay_attention_backward(q, k, v, log_decay, do, s0=None, dsn=None, lengths=
 
 def _rows(name, t):
     """(pointer, row stride) of a tensor seen as rows of its last dimension."""
-    shape, stride = t.shape, t.stride()
+    shape = t.shape
+    if t.is_contiguous():
+        return t.data_ptr(), shape[-1]
+    stride = t.stride()
     if shape[-1] > 1 and stride[-1] != 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
     if len(shape) == 1:
@@ -285,7 +290,8 @@ def add_norm(x, w, residual=None, eps=1e-6, p=0.0, seed=0, offset=0, out_dtype=N
              out: dict | None = None) -> dict:
     """h = residual + dropout(x), y = w h / sqrt(mean(h^2) + eps) (ambptt_add_norm): {"h", "y"}.
 
-    Rows are those of the last dimension; w fp32 [cols].  out_dtype "f8": y is
+    Rows are those of the last dimension; w fp32 [cols].  h is x itself where
+    nothing changes it (neither residual nor dropout).  out_dtype "f8": y is
     torch.float8_e4m3fn with "scale" fp32 [..., n] beside it, n = 1 scale per row
     or, with scale_block 128, one per 128 columns; y times its scale is the value.
     """
@@ -300,15 +306,20 @@ def add_norm(x, w, residual=None, eps=1e-6, p=0.0, seed=0, offset=0, out_dtype=N
         if residual is not None:
             _like("residual", residual, x.shape, x)
         _dense("w", w, (cols,), x, torch.float32)
-        h = _result(out, "h", x.shape, x)
+        drop = _drop(p, seed, offset)
+        same = residual is None and drop is None and not (out and out.get("h") is not None)
+        h = x if same else _result(out, "h", x.shape, x)
         y = _result(out, "y", x.shape, x, torch.float8_e4m3fn if f8 else None)
         res = {"h": h, "y": y}
         if f8:
             shape = (*x.shape[:-1], -(-cols // scale_block) if scale_block > 0 else 1)
             res["scale"] = _dense("scale", _result(out, "scale", shape, x, torch.float32), shape, x, torch.float32)
-        _check(load().ambptt_add_norm(C.byref(a), _drop(p, seed, offset), *_rows("x", x),
-                                      *(_rows("residual", residual) if residual is not None else (None, 0)),
-                                      _ptr(w), *_rows("h", h), *_rows("y", y), _ptr(res.get("scale")), _stream(x)))
+        xp, xl = _rows("x", x)
+        rp, rl = _rows("residual", residual) if residual is not None else (None, 0)
+        hp, hl = (None, 0) if same else _rows("h", h)
+        yp, yl = _rows("y", y)
+        _check(load().ambptt_add_norm(C.byref(a), drop, xp, xl, rp, rl, w.data_ptr(), hp, hl, yp, yl,
+                                      _ptr(res.get("scale")), _stream(x)))
     return res
 
 
