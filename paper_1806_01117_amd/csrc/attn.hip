@@ -34,8 +34,11 @@ namespace ambptt {
 
 namespace {
 
-constexpr int kC = 64;          // tokens per chunk
-constexpr int kRows = kC / 16;  // ... in tiles of 16
+// tokens per chunk, and in tiles of 16
+template <class T>
+constexpr int kChunk = sizeof(T) == 2 ? 64 : 32;
+template <class T>
+constexpr int kTileRows = kChunk<T> / 16;
 
 typedef unsigned int u4v __attribute__((ext_vector_type(4)));
 typedef unsigned int u2v __attribute__((ext_vector_type(2)));
@@ -221,12 +224,12 @@ struct Mm<float> {
   }
 };
 
-// 64 rows of NX elements on their way from memory to LDS
+// a chunk's rows of NX elements on their way from memory to LDS
 template <class T, int NX, int THREADS>
 struct Stage {
   static constexpr int kSize = int(sizeof(T)), kLanes = NX * kSize / 16;  // lanes per row
   static constexpr int kWaveRows = 64 / kLanes;                           // rows of a wave's load
-  static constexpr int kPer = THREADS / kLanes, kLoads = kC / kPer;       // rows of a load by all
+  static constexpr int kPer = THREADS / kLanes, kLoads = kChunk<T> / kPer;       // rows of a load by all
   u4v v[kLoads];
   __device__ __forceinline__ static int col(int id) { return id % kLanes * (16 / kSize); }
   // rows 0 .. m - 1 at p with the row stride `step` (elements), nx of their NX columns; the rest are zeros
@@ -235,7 +238,7 @@ struct Stage {
     const unsigned id = here(threadIdx.x);
     const char* const first = reinterpret_cast<const char*>(p + wave * kWaveRows * step);  // a wave's first row
     const unsigned from = (id % 64 / kLanes * unsigned(step) + col(id)) * kSize;
-    const bool whole = m == kC && nx == NX;
+    const bool whole = m == kChunk<T> && nx == NX;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       typedef __attribute__((address_space(1))) const u4u* Piece;
@@ -260,7 +263,7 @@ struct ChunkArgs {
   // Forwards c and out have G heads, backwards u and w.
   View c, u, w, out;
   int G, na, nb, H, nseg;   // na rows and nb columns of the state
-  int64_t T, L;             // tokens per segment, a multiple of kC
+  int64_t T, L;             // tokens per segment, a multiple of the chunk
   float scale;
   const float* log_decay;
   const int32_t* lengths;
@@ -314,15 +317,15 @@ __device__ __forceinline__ void store4(Global p, const f4& v) {
 
 // A chunk's factors, behind the tiles in LDS.
 struct Tables {
-  float power[kC];   // of a row's products: scale lambda^n, n tokens apart
-  float weight[kC];  // of the rows of the update: lambda^(m-1-j); backwards scale lambda^(j+1)
-  float from[kC];    // of the state in a row's result: scale lambda^(i+1); backwards lambda^(m-1-j)
+  float power[64];   // of a row's products: scale lambda^n, n tokens apart
+  float weight[64];  // of the rows of the update: lambda^(m-1-j); backwards scale lambda^(j+1)
+  float from[64];    // of the state in a row's result: scale lambda^(i+1); backwards lambda^(m-1-j)
 };
 
 template <class T, int NA, int NB>
 struct Plan {
   static constexpr int kWaves = NB / 16, kThreads = 64 * kWaves;
-  static constexpr int kUnits = kRows / Mm<T>::kTiles;                    // token units of a chunk
+  static constexpr int kC = kChunk<T>, kRows = kTileRows<T>, kUnits = kRows / Mm<T>::kTiles;                    // token units of a chunk
   static constexpr int kTileA = kC * tile_ld<T, NA>, kTileB = kC * tile_ld<T, NB>;
   static constexpr int kDots = kRows * kUnits * Mm<T>::kHalves * 1024;    // the exchanged products
   static constexpr int kLds = 2 * kTileA + kTileB + kDots + int(sizeof(Tables));
@@ -331,10 +334,10 @@ struct Plan {
 // S = whole S + the columns of u's tile in LDS times the rows w, each with its
 // weight: the parts FIRST .. LAST - 1 of those
 template <class T, int NA, int FIRST, int LAST, int AHEAD>
-__device__ __forceinline__ void update(f4 (&S)[NA / 16], float whole, typename Mm<T>::Frag (&w)[kRows / Mm<T>::kTiles],
+__device__ __forceinline__ void update(f4 (&S)[NA / 16], float whole, typename Mm<T>::Frag (&w)[kTileRows<T> / Mm<T>::kTiles],
                                        unsigned u, unsigned state_at, const float* weight) {
   typedef Mm<T> M;
-  constexpr int units = kRows / M::kTiles, ld = tile_ld<T, NA>;
+  constexpr int units = kTileRows<T> / M::kTiles, ld = tile_ld<T, NA>;
   const int g = here(threadIdx.x) % 64 / 16;
   typename M::Frag b[units][LAST], f[AHEAD][units];
 #pragma unroll
@@ -379,7 +382,7 @@ __global__ __launch_bounds__(64 * (NB / 16), sizeof(T) == 2 ? 4 : 2) void chunks
   extern __shared__ __align__(1024) char lds[];
   constexpr unsigned ct = 0, ut = P::kTileA, wt = 2 * P::kTileA, pt = wt + P::kTileB;
   Tables* const tab = reinterpret_cast<Tables*>(lds + pt + P::kDots);
-  constexpr int lda = tile_ld<T, NA>, ldb = tile_ld<T, NB>, TA = NA / 16, units = P::kUnits;
+  constexpr int lda = tile_ld<T, NA>, ldb = tile_ld<T, NB>, TA = NA / 16, units = P::kUnits, kC = P::kC, kRows = P::kRows;
   // fragments of LDS rows at a time: two of them take registers that the
   // backward kernels of the full size do not have
   constexpr int AHEAD = BACK && NA == 128 && sizeof(T) == 2 ? 1 : 2;
@@ -661,8 +664,9 @@ struct Cut {
   int nseg;
 };
 Cut cut(const AttnArgs& a) {
+  const int kC = a.bf16 ? kChunk<__bf16> : kChunk<float>;
   const int64_t chunks = (a.T + kC - 1) / kC, states = int64_t(a.B) * a.H;
-  int64_t want = (a.dk > 64 || a.dv > 64 ? 256 : 512) / states;
+  int64_t want = states >= 192 ? 1 : 512 / states;
   if (want > chunks / 2) want = chunks / 2;  // a segment of one chunk would only move states
   if (want < 1) want = 1;
   const int64_t per = chunks ? (chunks + want - 1) / want : 1;
