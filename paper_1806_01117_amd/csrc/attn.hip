@@ -375,7 +375,7 @@ __device__ __forceinline__ void update(f4 (&S)[NA / 16], float whole, typename M
 // result (sn).  ONE: the group has one head (what passes from head to head
 // takes no registers).
 template <class T, int NA, int NB, bool BACK, bool OUT, bool EXACT, bool ONE>
-__global__ __launch_bounds__(64 * (NB / 16), sizeof(T) == 2 ? 4 : 2) void chunks(Work job) {
+__global__ __launch_bounds__(64 * (NB / 16), 4) void chunks(Work job) {
   typedef Mm<T> M;
   typedef Plan<T, NA, NB> P;
   typedef typename M::Frag Frag;
@@ -384,8 +384,8 @@ __global__ __launch_bounds__(64 * (NB / 16), sizeof(T) == 2 ? 4 : 2) void chunks
   Tables* const tab = reinterpret_cast<Tables*>(lds + pt + P::kDots);
   constexpr int lda = tile_ld<T, NA>, ldb = tile_ld<T, NB>, TA = NA / 16, units = P::kUnits, kC = P::kC, kRows = P::kRows;
   // fragments of LDS rows at a time: two of them take registers that the
-  // backward kernels of the full size do not have
-  constexpr int AHEAD = BACK && NA == 128 && sizeof(T) == 2 ? 1 : 2;
+  // kernels of the full size do not have
+  constexpr int AHEAD = NA == 128 && (BACK || sizeof(T) == 4) ? 1 : 2;
 
   const int id = job.kinds == 1 ? blockIdx.x : blockIdx.x / 16 * 8 + blockIdx.x % 8;
   if (id >= job.each) return;
@@ -658,7 +658,13 @@ hipError_t launch_chunks(const ChunkArgs& a, const ChunkArgs* b, int bf16, int B
   }
 }
 
-// Tokens per segment and segments: as many workgroups as the CUs hold at once.
+// Tokens per segment, and segments: the number with the least time by what a
+// chunk takes a workgroup, in us: 6 alone on its CU and 9.5 beside another, 2.5
+// in the launch that forms the segments' own states, and, for more than one
+// segment, 8 for the launches and the states' passage at 4 TB/s (8 bytes for
+// each of their values).  Measured against one segment, bf16, 128 x 128: 8
+// states of 20000 tokens 164 us in 63 segments (187 in 32), 256 states of 10000
+// 2.15 ms for the gradients in one (2.53 in two).
 struct Cut {
   int64_t L;
   int nseg;
@@ -666,11 +672,15 @@ struct Cut {
 Cut cut(const AttnArgs& a) {
   const int kC = a.bf16 ? kChunk<__bf16> : kChunk<float>;
   const int64_t chunks = (a.T + kC - 1) / kC, states = int64_t(a.B) * a.H;
-  int64_t want = states >= 192 ? 1 : 512 / states;
-  if (want > chunks / 2) want = chunks / 2;  // a segment of one chunk would only move states
-  if (want < 1) want = 1;
-  const int64_t per = chunks ? (chunks + want - 1) / want : 1;
-  return {per * kC, int(chunks ? (chunks + per - 1) / per : 1)};
+  int64_t best = chunks > 0 ? chunks : 1;  // chunks per segment: one segment
+  double least = double(best) * ((states + 511) / 512) * (states > 256 ? 9.5 : 6.0);
+  for (int64_t per = 1; per < chunks; per += per < 8 ? 1 : per / 8) {
+    const int64_t all = states * ((chunks + per - 1) / per);
+    if (all > 512) continue;  // a second round of workgroups
+    const double us = per * ((all > 256 ? 9.5 : 6.0) + 2.5) + 8.0 + double(all) * a.dk * a.dv * 8 / 4e6;
+    if (us < least) least = us, best = per;
+  }
+  return {best * kC, int(chunks ? (chunks + best - 1) / best : 1)};
 }
 
 size_t states_bytes(const AttnArgs& a, const Cut& c) {
