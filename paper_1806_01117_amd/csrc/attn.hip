@@ -166,7 +166,7 @@ struct Mm<__bf16> {
     for (int i = 0; i < 4; ++i) {
       const float x = p[i / 2][i % 2 * 2], y = p[i / 2][i % 2 * 2 + 1];
       a[i] = pk_bf16(x, y);
-      b[i] = pk_bf16(less_lo(x, a[i]), less_hi(y, a[i]));
+      b[i] = pk_bf16(x - lo_f(a[i]), y - hi_f(a[i]));
     }
     out[0] = __builtin_bit_cast(Frag, a), out[1] = __builtin_bit_cast(Frag, b);
   }
@@ -332,41 +332,45 @@ struct Plan {
 };
 
 // S = whole S + the columns of u's tile in LDS times the rows w, each with its
-// weight: the parts FIRST .. LAST - 1 of those
-template <class T, int NA, int FIRST, int LAST, int AHEAD>
+// weight and split in PARTS; GO units at a time, so that no more than their
+// parts are in registers
+template <class T, int NA, int PARTS, int AHEAD, int GO>
 __device__ __forceinline__ void update(f4 (&S)[NA / 16], float whole, typename Mm<T>::Frag (&w)[kTileRows<T> / Mm<T>::kTiles],
-                                       unsigned u, unsigned state_at, const float* weight) {
+                                       unsigned state_at, const float* weight) {
   typedef Mm<T> M;
   constexpr int units = kTileRows<T> / M::kTiles, ld = tile_ld<T, NA>;
-  const int g = here(threadIdx.x) % 64 / 16;
-  typename M::Frag b[units][LAST], f[AHEAD][units];
 #pragma unroll
-  for (int i = 0; i < units; ++i) {
-    float by[4 * M::kTiles];
+  for (int u = 0; u < units; u += GO) {
+    const int g = here(threadIdx.x) % 64 / 16;
+    typename M::Frag b[GO][PARTS], f[AHEAD][GO];
 #pragma unroll
-    for (int k = 0; k < M::kTiles; ++k) {
-      const f4 v = *(const f4*)(weight + 16 * (M::kTiles * i + k) + 4 * g);
+    for (int i = 0; i < GO; ++i) {
+      float by[4 * M::kTiles];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) by[4 * k + r] = v[r];
+      for (int k = 0; k < M::kTiles; ++k) {
+        const f4 v = *(const f4*)(weight + 16 * (M::kTiles * (u + i) + k) + 4 * g);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) by[4 * k + r] = v[r];
+      }
+      M::split(w[u + i], by, b[i]);
     }
-    M::split(w[i], by, b[i]);
-  }
-  auto columns = [&](int d) {
-    const unsigned at = M::state_tile(state_at, d);
+    auto columns = [&](int d) {
+      const unsigned at = M::state_tile(state_at, d);
 #pragma unroll
-    for (int i = 0; i < units; ++i) f[d % AHEAD][i] = M::token(at + u, ld, i);
-  };
-  if (AHEAD > 1) columns(0);
+      for (int i = 0; i < GO; ++i) f[d % AHEAD][i] = M::token(at + Plan<T, NA, NA>::kTileA, ld, u + i);
+    };
+    if (AHEAD > 1) columns(0);
 #pragma unroll
-  for (int d = 0; d < NA / 16; ++d) {
-    if (AHEAD == 1 || d + 1 < NA / 16) columns(AHEAD == 1 ? d : d + 1);  // two: on their way during this tile's products
-    f4 sum = {0, 0, 0, 0};
+    for (int d = 0; d < NA / 16; ++d) {
+      if (AHEAD == 1 || d + 1 < NA / 16) columns(AHEAD == 1 ? d : d + 1);  // two: on their way during this tile's products
+      f4 sum = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < units; ++i)
+      for (int i = 0; i < GO; ++i)
 #pragma unroll
-      for (int p = LAST - 1; p >= FIRST; --p) sum = M::mul(f[d % AHEAD][i], b[i][p], sum);
+        for (int p = PARTS - 1; p >= 0; --p) sum = M::mul(f[d % AHEAD][i], b[i][p], sum);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) S[d][r] = fmaf(whole, S[d][r], sum[r]);
+      for (int r = 0; r < 4; ++r) S[d][r] = u ? S[d][r] + sum[r] : fmaf(whole, S[d][r], sum[r]);
+    }
   }
 }
 
@@ -407,7 +411,7 @@ __global__ __launch_bounds__(64 * (NB / 16), 4) void chunks(Work job) {
   // this lane's addresses in LDS: row fragments, columns of the state's rows
   // and of its own columns, pieces on their way there, exchanged products
   const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds;
-  const unsigned row_at = base + tile_at<T, NA>(n, 16 * g), state_at = M::template state_at<NA>();
+  const unsigned row_at = base + tile_at<T, NA>(n, 16 * g), state_at = base + M::template state_at<NA>();
   Stage<T, NA, P::kThreads> sc, su;
   Stage<T, NB, P::kThreads> sw;
   auto fetch = [&](int64_t t, int q) {
@@ -556,14 +560,8 @@ __global__ __launch_bounds__(64 * (NB / 16), 4) void chunks(Work job) {
       if (BACK || q + 1 == heads) {
         // S = lambda^m S + sum of u (weight w)^T
         const float whole = BACK && q ? 1.0f : m == kC ? full : power(ld, m);
-        if constexpr (EXACT && BACK && OUT && M::kParts == 3) {
-          // in two goes: the fragments of all three parts at once would push
-          // the rows on their way out of the registers
-          update<T, NA, 2, 3, AHEAD>(S, whole, w, base + ut, state_at, tab->weight);
-          update<T, NA, 0, 2, AHEAD>(S, 1.0f, w, base + ut, state_at, tab->weight);
-        } else {
-          update<T, NA, 0, EXACT || M::kParts == 1 ? M::kParts : 2, AHEAD>(S, whole, w, base + ut, state_at, tab->weight);
-        }
+        constexpr int go = EXACT && BACK && OUT && M::kParts == 3 ? 1 : units;
+        update<T, NA, EXACT || M::kParts == 1 ? M::kParts : 2, AHEAD, go>(S, whole, w, state_at, tab->weight);
       }
       __syncthreads();
     }
