@@ -170,6 +170,13 @@ struct Mm<__bf16> {
     }
     out[0] = __builtin_bit_cast(Frag, a), out[1] = __builtin_bit_cast(Frag, b);
   }
+  // adds zeros to `odd`, and a NaN for values that are not finite
+  static __device__ __forceinline__ float not_finite(const Frag& x, float odd) {
+    const u4v v = __builtin_bit_cast(u4v, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) odd = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, v[i]), bf16x2{0, 0}, odd, false);
+    return odd;
+  }
   // x times the weights, in parts of 8 bits: three hold all of them
   template <int PARTS>
   static __device__ __forceinline__ void split(const Frag& x, const float (&w)[8], Frag (&out)[PARTS]) {
@@ -218,6 +225,11 @@ struct Mm<float> {
   }
   static __device__ __forceinline__ unsigned state_tile(unsigned at, int t) { return flip(at, 64 * t); }
   static __device__ __forceinline__ void pack(const f4 (&p)[1], Frag (&out)[1]) { out[0] = p[0]; }
+  static __device__ __forceinline__ float not_finite(const Frag& x, float odd) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) odd = fmaf(x[r], 0.0f, odd);
+    return odd;
+  }
   static __device__ __forceinline__ void split(const Frag& x, const float (&w)[4], Frag (&out)[1]) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) out[0][r] = x[r] * w[r];
@@ -329,6 +341,8 @@ struct Plan {
   static constexpr int kTileA = kC * tile_ld<T, NA>, kTileB = kC * tile_ld<T, NB>;
   static constexpr int kDots = kRows * kUnits * Mm<T>::kHalves * 1024;    // the exchanged products
   static constexpr int kLds = 2 * kTileA + kTileB + kDots + int(sizeof(Tables));
+  // waves of a SIMD: four, and as many workgroups as LDS holds where they have one to each
+  static constexpr int kSimd = kWaves > 4 || 163840 / kLds > 4 ? 4 : 163840 / kLds;
 };
 
 // S = whole S + the columns of u's tile in LDS times the rows w, each with its
@@ -379,7 +393,7 @@ __device__ __forceinline__ void update(f4 (&S)[NA / 16], float whole, typename M
 // result (sn).  ONE: the group has one head (what passes from head to head
 // takes no registers).
 template <class T, int NA, int NB, bool BACK, bool OUT, bool EXACT, bool ONE>
-__global__ __launch_bounds__(64 * (NB / 16), 4) void chunks(Work job) {
+__global__ __launch_bounds__(64 * (NB / 16), (Plan<T, NA, NB>::kSimd)) void chunks(Work job) {
   typedef Mm<T> M;
   typedef Plan<T, NA, NB> P;
   typedef typename M::Frag Frag;
@@ -389,7 +403,7 @@ __global__ __launch_bounds__(64 * (NB / 16), 4) void chunks(Work job) {
   constexpr int lda = tile_ld<T, NA>, ldb = tile_ld<T, NB>, TA = NA / 16, units = P::kUnits, kC = P::kC, kRows = P::kRows;
   // fragments of LDS rows at a time: two of them take registers that the
   // kernels of the full size do not have
-  constexpr int AHEAD = NA == 128 && (BACK || sizeof(T) == 4) ? 1 : 2;
+  constexpr int AHEAD = P::kSimd == 4 && NA == 128 && (BACK || EXACT || sizeof(T) == 4) ? 1 : 2;
 
   const int id = job.kinds == 1 ? blockIdx.x : blockIdx.x / 16 * 8 + blockIdx.x % 8;
   if (id >= job.each) return;
@@ -521,6 +535,38 @@ __global__ __launch_bounds__(64 * (NB / 16), 4) void chunks(Work job) {
       for (int u = 0; u < units; ++u) w[u] = M::token(own_at, ldb, u);
       if (OUT) {
         const unsigned dot_at = base + pt + here(threadIdx.x) % 64 * 16;
+        float odd = 0.0f;
+#pragma unroll
+        for (int u = 0; u < units; ++u) odd = M::not_finite(w[u], odd);
+        const bool poison = __any(odd != odd);
+        if (poison) {
+          // A zero of the causal mask times an infinity or a NaN is a NaN, in
+          // tokens that the formula keeps clear of it: such values are zeros
+          // here, and the tokens that have one on their side are NaN.
+#pragma unroll
+          for (int u = 0; u < units; ++u) {
+            Frag bad;
+#pragma unroll
+            for (int i = 0; i < 4 * M::kTiles; ++i) {
+              const float f = float(w[u][i]) * 0.0f;
+              bad[i] = f == 0.0f ? 0.0f : 1.0f;
+              w[u][i] = f == 0.0f ? float(w[u][i]) : 0.0f;
+            }
+#pragma unroll
+            for (int it = 0; it < kRows; ++it) {
+              const unsigned l = here(threadIdx.x) % 64;
+              Frag side;
+#pragma unroll
+              for (int i = 0; i < 4 * M::kTiles; ++i) {
+                const int far = 16 * (it - M::kTiles * u - i / 4) - i % 4 + int(l % 16) - int(l / 16) * 4;
+                side[i] = (BACK ? -far : far) >= 0 ? 1.0f : 0.0f;
+              }
+              const f4 hits = M::mul(bad, side, f4{0, 0, 0, 0});
+#pragma unroll
+              for (int r = 0; r < 4; ++r) o[it][r] = hits[r] > 0.0f ? __builtin_nanf("") : o[it][r];
+            }
+          }
+        }
 #pragma unroll
         for (int u = 0; u < units; ++u) {
 #pragma unroll
@@ -534,6 +580,10 @@ __global__ __launch_bounds__(64 * (NB / 16), 4) void chunks(Work job) {
             for (int it = 0; it < kRows; ++it)
               if (BACK ? M::kTiles * u + M::kTiles - 1 >= it : M::kTiles * u <= it) o[it] = M::mul(w[u], p[it], o[it]);
           }
+        }
+        if (poison) {  // the state takes them as they are
+#pragma unroll
+          for (int u = 0; u < units; ++u) w[u] = M::token(own_at, ldb, u);
         }
         // The next rows are in registers by now.  Waited for here, before the
         // stores, which the same counter counts, they need no wait that would
@@ -560,7 +610,7 @@ __global__ __launch_bounds__(64 * (NB / 16), 4) void chunks(Work job) {
       if (BACK || q + 1 == heads) {
         // S = lambda^m S + sum of u (weight w)^T
         const float whole = BACK && q ? 1.0f : m == kC ? full : power(ld, m);
-        constexpr int go = EXACT && BACK && OUT && M::kParts == 3 ? 1 : units;
+        constexpr int go = P::kSimd == 4 && NA == 128 && OUT && EXACT ? 1 : units;
         update<T, NA, EXACT || M::kParts == 1 ? M::kParts : 2, AHEAD, go>(S, whole, w, state_at, tab->weight);
       }
       __syncthreads();
@@ -631,8 +681,9 @@ hipError_t run_form(const Work& job, hipStream_t s) {
 
 template <class T, int NA, int NB, bool BACK, bool OUT>
 hipError_t run_chunks(const Work& job, hipStream_t s) {
-  // fp32 kernels have no form for states that are no result: they split nothing
-  constexpr bool split = OUT && Mm<T>::kParts > 1;
+  // Only forwards in bf16 is there a form for states that are no result: fp32
+  // splits nothing, and backwards it saved nothing beside its partner.
+  constexpr bool split = OUT && !BACK && Mm<T>::kParts > 1;
   const bool one = OUT && job.a[0].G == 1;
   if (split && !job.a[0].sn)
     return one ? run_form<T, NA, NB, BACK, OUT, !split, OUT>(job, s) : run_form<T, NA, NB, BACK, OUT, !split, false>(job, s);

@@ -203,6 +203,39 @@ def test_attention_few_and_many_rows(amb, dtype, B, T, H):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,T,H,G,dk,dv", [(2, 150, 2, 2, 64, 64), (1, 1000, 1, 1, 128, 128), (1, 90, 3, 1, 32, 112)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_attention_keeps_infinities_to_their_side(amb, dtype, B, T, H, G, dk, dv, value):
+    """A value at token j is in the results that depend on it, and in no others: those keep every bit."""
+    torch = _torch()
+    j = 69
+    clean = Attn(dtype, B, T, H, G, dk, dv)
+    want = dict(amb.decay_attention(*clean.args, s0=clean.s0d, **clean.more))
+    want.update(amb.decay_attention_backward(*clean.args, clean.dev["do"], s0=clean.s0d, dsn=clean.dsnd, **clean.more))
+    # by operand: the results' tokens that see it, of o, dq, dk and dv
+    before, own, after, none = slice(0, j + 1), slice(j, j + 1), slice(j, T), slice(0, 0)
+    seen = dict(q=dict(o=own, dq=none, dk=before, dv=before), k=dict(o=after, dq=after, dk=none, dv=own),
+                v=dict(o=after, dq=after, dk=own, dv=none), do=dict(o=none, dq=own, dk=before, dv=before))
+    for name, sides in seen.items():
+        c = Attn(dtype, B, T, H, G, dk, dv)
+        c.dev[name][-1, j, 0, 5] = value
+        got = dict(amb.decay_attention(*c.args, s0=c.s0d, **c.more))
+        got.update(amb.decay_attention_backward(*c.args, c.dev["do"], s0=c.s0d, dsn=c.dsnd, **c.more))
+        for r, side in sides.items():
+            free = torch.ones(got[r].shape[1], dtype=torch.bool)
+            free[side] = False
+            heads = range(G) if r in ("o", "dq") and name in "kv" else [0]
+            for h in range(got[r].shape[2]):
+                if h not in heads:
+                    assert torch.equal(got[r][-1, :, h], want[r][-1, :, h]), (name, r, h)
+                    continue
+                assert torch.equal(got[r][-1, free, h], want[r][-1, free, h]), (name, r, h)
+                hit = ~torch.isfinite(got[r][-1, ~free, h])
+                assert hit.any(-1).all(), (name, r, h)
+            assert torch.equal(got[r][:-1], want[r][:-1]), (name, r)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_attention_decays_at_their_ends(amb, dtype):
     # no memory at all (lambda = 0), next to none, and without end
     c = Attn(dtype, 1, 140, 4, 1, 32, 32, decays=[-float("inf"), -80.0, 0.0, -1e-6])
