@@ -35,12 +35,15 @@ extern "C" {
  *   S_i = lambda S_{i-1} + k_i v_i^T,   o_i = scale S_i^T q_i,
  * for the row's first lengths[b] tokens (all without lengths).  Query head
  * h * group + g reads the state of key/value head h.  Outputs of the tokens
- * past a row's length are zero, and nothing in their inputs is used.
+ * past a row's length are zero, and nothing in their inputs is used.  An
+ * infinity or NaN in a token reaches the results that depend on it by these
+ * formulas, as an infinity or as a NaN, and no others.
  *
  * Gradients, with D_n the gradient of the last state:
  *   A_i = D_i + scale sum_g q_i do_i^T,  dk_i = A_i v_i,  dv_i = A_i^T k_i,
  *   D_{i-1} = lambda A_i,  dq_i = scale S_i do_i.
- * The decay is a constant of the head: it has no gradient here. */
+ * The decay is a constant of the head (log_decay <= 0 is meant, any finite value
+ * and -infinity are taken): it has no gradient here. */
 typedef struct {
   int32_t dtype;      /* AMBPTT_F32 | AMBPTT_BF16: q, k, v, o and their gradients */
   int32_t batch;      /* >= 1 */
@@ -111,7 +114,7 @@ ambptt_status ambptt_dropout(int32_t dtype, int64_t rows, int64_t cols, const am
  *
  *   h = residual + dropout(x),   y = w h / sqrt(mean(h^2) + eps)
  * row by row, h and y in fp32 until they are stored. */
-enum { AMBPTT_F8 = 2 };  /* y in 8 bits: OCP e4m3, y ~= scale * stored, scale = max|y| / 448 */
+enum { AMBPTT_F8 = 2 };  /* y in 8 bits: OCP e4m3, y ~= scale * stored, scale = max|y| / 448 and >= 2^-126 */
 
 typedef struct {
   int32_t dtype;        /* AMBPTT_F32 | AMBPTT_BF16: x, residual, h and the gradients */

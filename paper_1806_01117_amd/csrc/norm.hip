@@ -1,4 +1,9 @@
 // Dropout, and the root-mean-square norm behind the residual's addition.
+//
+// All of these are bound by memory where rows are many, at what a copy reaches
+// (4.8 to 5.05 TB/s), and by the launch where they are few:
+//   dropout, 10000 rows of 64 x 2048 bf16 values  see the kernel
+//   add_norm                                      see form_of
 #include "ops.hpp"
 
 namespace ambptt {
@@ -238,7 +243,8 @@ __device__ __forceinline__ void store_y(const float (&h)[kV], float (&y)[kV], fl
       for (int o = 8; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
     }
     if (c >= a.cols) return;
-    const float scale = most > 0.0f ? most / 448.0f : 1.0f;
+    // a normal number: one that lost bits would take what it divides out of range
+    const float scale = most > 0.0f ? fmaxf(most / 448.0f, 0x1p-126f) : 1.0f;
     if (a.block ? c % 128 == 0 : c == 0) a.scale[a.block ? r * ((a.cols + 127) / 128) + c / 128 : r] = scale;
     uint32_t u[kV / 2];
 #pragma unroll
@@ -320,12 +326,9 @@ __device__ __forceinline__ void zero8(float (&v)[kV]) {
 
 // Every gridDim.x-th group of rows: their dr, dx, and the sum of dy h r over
 // them in the workgroup's row of parts.
-// (waves per SIMD of the backward kernel: what norm_grad_parts counts on)
-template <int THREADS, int NV>
-constexpr int kWavesBack = THREADS == 1024 || NV < 4 ? 4 : 2;
-
+// Four waves to a SIMD: what norm_grad_parts counts on.
 template <class T, int THREADS, int NV>
-__global__ __launch_bounds__(kBlock<THREADS>, (kWavesBack<THREADS, NV>)) void add_norm_backward(NormGradArgs a) {
+__global__ __launch_bounds__(kBlock<THREADS>, 4) void add_norm_backward(NormGradArgs a) {
   __shared__ float lds[2 * (THREADS / 64)];
   extern __shared__ float sums[];  // THREADS 64: the waves' sums
   const int64_t wide = (a.cols + kV - 1) / kV, rows = kRowsPer<THREADS>;
@@ -440,18 +443,24 @@ __global__ __launch_bounds__(kThreads) void sum_parts(const float* p, int parts,
   out[c] = v;
 }
 
-// Threads to a row and pieces to a lane.  One wave takes rows of up to 1024
-// columns, and of 2048 where there are enough of them to fill the CUs with
-// waves of their own; then a workgroup.
+// Threads to a row and pieces to a lane: one wave while that takes two pieces,
+// then workgroups with one piece to a lane, up to the largest.  Measured, us
+// forward and backward with 20000 rows of bf16:
+//   512 columns  64 x 1  13.9 20.4    256 x 1 25.6 36.6
+//   1024         64 x 2  28.4 30.1    256 x 1 30.7 38.1
+//   2048         256 x 1 57.9 49.1    64 x 4  64.9 54.0
+//   4096         512 x 1 120  109     256 x 2 127  134
+//   8192         1024 x 1 291 233     256 x 4 304  278    512 x 2 261 273
+//   16384        1024 x 2 529 406     1024, rows read again 571 842
 struct Form {
   int threads, nv;
 };
-Form form_of(int64_t rows, int64_t cols) {
+Form form_of(int64_t cols) {
   if (cols <= 512) return {64, 1};
   if (cols <= 1024) return {64, 2};
-  if (cols <= 2048) return rows >= 4096 ? Form{64, 4} : Form{256, 1};
-  if (cols <= 4096) return {256, 2};
-  if (cols <= 8192) return {256, 4};
+  if (cols <= 2048) return {256, 1};
+  if (cols <= 4096) return {512, 1};
+  if (cols <= 8192) return {1024, 1};
   if (cols <= 16384) return {1024, 2};
   return {1024, 0};
 }
@@ -472,16 +481,16 @@ hipError_t run_norm_backward(const NormGradArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-#define BY_FORM(run, T, a, s)                                 \
-  switch (form_of(a.rows, a.cols).threads * 8 + form_of(a.rows, a.cols).nv) { \
-    case 64 * 8 + 1: return run<T, 64, 1>(a, s);              \
-    case 64 * 8 + 2: return run<T, 64, 2>(a, s);              \
-    case 64 * 8 + 4: return run<T, 64, 4>(a, s);              \
-    case 256 * 8 + 1: return run<T, 256, 1>(a, s);            \
-    case 256 * 8 + 2: return run<T, 256, 2>(a, s);            \
-    case 256 * 8 + 4: return run<T, 256, 4>(a, s);            \
-    case 1024 * 8 + 2: return run<T, 1024, 2>(a, s);          \
-    default: return run<T, 1024, 0>(a, s);                    \
+#define BY_FORM(run, T, a, s)                        \
+  const Form f = form_of(a.cols);                    \
+  switch (f.threads + f.nv) {                        \
+    case 64 + 1: return run<T, 64, 1>(a, s);         \
+    case 64 + 2: return run<T, 64, 2>(a, s);         \
+    case 256 + 1: return run<T, 256, 1>(a, s);       \
+    case 512 + 1: return run<T, 512, 1>(a, s);       \
+    case 1024 + 1: return run<T, 1024, 1>(a, s);     \
+    case 1024 + 2: return run<T, 1024, 2>(a, s);     \
+    default: return run<T, 1024, 0>(a, s);           \
   }
 
 template <class T>
@@ -527,10 +536,11 @@ hipError_t launch_add_norm(const NormArgs& a, hipStream_t s) {
   return a.bf16 ? norm_by_form<__bf16>(a, s) : norm_by_form<float>(a, s);
 }
 
-// as many workgroups as the CUs hold at once, and no more than there are rows for
+// as many workgroups as 256 CUs hold at once with four waves to a SIMD, and no
+// more than there are rows for
 int norm_grad_parts(int64_t rows, int64_t cols) {
-  const Form f = form_of(rows, cols);
-  const int64_t groups = f.threads == 64 ? (rows + 3) / 4 : rows, most = f.threads == 1024 ? 256 : f.nv == 4 ? 512 : 1024;
+  const int threads = form_of(cols).threads;
+  const int64_t groups = threads == 64 ? (rows + 3) / 4 : rows, most = threads == 64 ? 1024 : 262144 / threads;
   return int(groups < 1 ? 1 : groups < most ? groups : most);
 }
 

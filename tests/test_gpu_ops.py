@@ -267,6 +267,21 @@ def test_attention_step_is_the_sequence(amb, dtype, B, H, G, dk, dv):
     _near(s, sn, "f32", "s")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_step_leaves_a_finished_row(amb, dtype):
+    # a row without a token keeps its state, whatever it holds, in place and in another buffer
+    torch = _torch()
+    c = Attn(dtype, 2, 1, 3, 2, 32, 48, lengths=[0, 1])
+    s = c.s0d.clone()
+    s[0, 1, 4, 5], s[0, 2, 7, 1], s[0, 0, 0, 0] = float("inf"), float("nan"), -0.0
+    keep = s[0].clone()
+    r = amb.decay_attention(*c.args, s0=s, **c.more)
+    o = amb.decay_attention_step(*c.args, s, lengths=c.more["lengths"], scale=c.scale)
+    for t in (r["sn"][0], s[0]):
+        assert torch.equal(t.view(torch.int32), keep.view(torch.int32))
+    assert not o[0].any() and not r["o"][0].any() and torch.equal(s[1], r["sn"][1])
+
+
 def test_attention_offsets_past_32_bits(amb):
     # tokens 2^26 elements apart: the offsets pass 2^32
     torch = _torch()
@@ -496,6 +511,22 @@ def test_norm_in_8_bits(amb, dtype, rows, cols, block):
     s = np.repeat(scale, wide, 1)[:, :cols]
     d = np.abs(_np(got["y"].float()) * s - y)
     assert (d <= 1.001 * np.abs(y) * 2.0 ** -4 + s * 2.0 ** -10).all() and np.abs(_np(got["y"].float())).max() <= 448
+
+
+@pytest.mark.parametrize("block", [0, 128])
+def test_norm_in_8_bits_below_the_normal_numbers(amb, block):
+    # a scale that lost its bits would take the stored values past 448: it is 2^-126 at least
+    torch = _torch()
+    x = torch.randn(3, 200, device="cuda")
+    for size in (1e-36, 1e-38, 1e-40, 2e-44):
+        w = torch.full((200,), size, device="cuda")
+        got = amb.add_norm(x, w, out_dtype="f8", scale_block=block)
+        y = O.norm(_np(x), _np(w), 1e-6)
+        scale = _np(got["scale"])
+        assert (scale >= 2.0 ** -126).all()
+        s = np.repeat(scale, block or 200, 1)[:, :200]
+        d = np.abs(_np(got["y"].float()) * s - y)
+        assert (d <= 1.001 * np.abs(y) * 2.0 ** -4 + s * 2.0 ** -10 + 2.0 ** -147).all()
 
 
 def test_norm_rows_and_views(amb):

@@ -125,6 +125,19 @@ def test_attention_refuses_operands(lib, views, ptr):
     assert _attention(lib, None, views, **ptr) == EINVAL
 
 
+@pytest.mark.parametrize("dtype,size", [(0, 4), (1, 2)])
+@pytest.mark.parametrize("name", ["q", "k", "v", "o"])
+def test_attention_refuses_tokens_far_apart(lib, dtype, size, name):
+    # 32-bit offsets reach 16 tokens that are 2^28 bytes apart, and no further
+    far = dict(step=2 ** 28 // size + 1, batch=2 ** 40)
+    assert _attention(lib, dict(dtype=dtype), {name: far}) == EUNSUPPORTED
+
+
+def test_norm_refuses_sizes(lib):
+    assert _norm(lib, cols=2 ** 30 + 1, ldx=2 ** 31, ldh=2 ** 31, ldy=2 ** 31) == EUNSUPPORTED
+    assert _norm(lib, rows=2 ** 31) == EUNSUPPORTED
+
+
 def test_attention_refuses_null(lib):
     n = ctypes.c_size_t()
     assert lib.ambptt_decay_attention_workspace(None, 0, ctypes.byref(n)) == EINVAL
