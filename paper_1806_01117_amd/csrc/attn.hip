@@ -1,4 +1,4 @@
-// Attention whose state decays, in chunks of 64 tokens on the matrix cores.
+// Attention whose state decays, in chunks of tokens on the matrix cores.
 //
 // With lambda^(i-j) between the tokens of a chunk and the state S before it,
 //   o_i = sum_{j <= i} lambda^(i-j) (q_i . k_j) v_j + lambda^(i+1) S^T q_i,
@@ -18,6 +18,21 @@
 // operands of the product with q as they stand, and nothing of the state passes
 // through LDS; the products q k^T are shared out over the waves and exchanged
 // there.
+//
+// Chunks have 64 tokens in bf16 and 32 in fp32.  Longer ones take more products
+// inside the chunk and more LDS, shorter ones more passes over the state: bf16
+// 64 against 32, 164 and 172 us (a prompt of 20000 tokens, 8 states of 128 x 128,
+// 32 query heads) and 2154 and 2345 us (gradients of 256 such states over 10000
+// tokens); fp32 64 against 32, 668 and 530 us (64 rows of 1000 tokens, 8 states
+// of 64 x 64, with the gradients), since two workgroups of 64 do not fit a CU.
+//
+// What bounds them.  The gradients above take 2.1 ms, 2.2 TB/s of what has to
+// move: dk and dv 1387 us with two workgroups to a CU, where vector
+// instructions take 62 % of a SIMD's time and matrix instructions 39 %, that is
+// all of it; dq 821 us with one workgroup to a CU, 46 % and 27 %, the rest being
+// what its waves wait for each other at the two barriers of a chunk.  The prompt
+// takes 166 us, 2.5 TB/s, 52 % and 28 % in the launch that writes the results.
+// In fp32 matrix instructions alone take 53 % (forwards) and 65 % (backwards).
 //
 // Rounding.  States, accumulators and sums are fp32, and bf16 operands enter
 // the matrix cores as they are.  The fp32 values that go there in the bf16
@@ -55,8 +70,9 @@ __device__ __forceinline__ unsigned pk_bf16(float a, float b) {
 }
 __device__ __forceinline__ float lo_f(unsigned p) { return __builtin_bit_cast(float, p << 16); }
 __device__ __forceinline__ float hi_f(unsigned p) { return __builtin_bit_cast(float, p & 0xffff0000u); }
-// x minus the low (the high) value of a pair, exactly where the pair rounded x:
-// a product of pairs with (-1, 0) or (0, -1), one instruction where unpacking
+// x minus the low (the high) value of a pair, exactly where the pair rounded x
+// (for a chain of such pairs; a single one is unpacked and subtracted while
+// another wave's products run): a product of pairs with (-1, 0) or (0, -1), one instruction where unpacking
 // and subtracting take two.  The factors come from a register: written as the
 // constant -1.0 the pair (-1, 0) reaches the instruction as (0, -1).
 __device__ __forceinline__ float less_lo(float x, unsigned p) {
@@ -347,7 +363,7 @@ struct Plan {
 
 // S = whole S + the columns of u's tile in LDS times the rows w, each with its
 // weight and split in PARTS; GO units at a time, so that no more than their
-// parts are in registers
+// parts are in registers (AHEAD: fragments of u on their way)
 template <class T, int NA, int PARTS, int AHEAD, int GO>
 __device__ __forceinline__ void update(f4 (&S)[NA / 16], float whole, typename Mm<T>::Frag (&w)[kTileRows<T> / Mm<T>::kTiles],
                                        unsigned state_at, const float* weight) {
@@ -390,8 +406,15 @@ __device__ __forceinline__ void update(f4 (&S)[NA / 16], float whole, typename M
 
 // Results of a segment's tokens (OUT), or the state that the segment alone
 // leaves.  BACK: from the last token to the first.  EXACT: the last state is a
-// result (sn).  ONE: the group has one head (what passes from head to head
-// takes no registers).
+// result (sn), and the weighted rows are split in three (see above).  ONE: the
+// group has one head (what passes from head to head takes no registers).  Both
+// are of the compiler's, not of the run: a kernel that could do either held
+// registers for both and spilled, 4 ms for the gradients above.
+//
+// Four waves to a SIMD have 128 registers each.  State, chunk on its way and
+// results take 72 of them, so what else is live is kept small where that is
+// tight (128 rows): one fragment ahead in place of two, one unit of the exact
+// update in place of all, addresses that are formed where they are used.
 template <class T, int NA, int NB, bool BACK, bool OUT, bool EXACT, bool ONE>
 __global__ __launch_bounds__(64 * (NB / 16), (Plan<T, NA, NB>::kSimd)) void chunks(Work job) {
   typedef Mm<T> M;
@@ -401,8 +424,7 @@ __global__ __launch_bounds__(64 * (NB / 16), (Plan<T, NA, NB>::kSimd)) void chun
   constexpr unsigned ct = 0, ut = P::kTileA, wt = 2 * P::kTileA, pt = wt + P::kTileB;
   Tables* const tab = reinterpret_cast<Tables*>(lds + pt + P::kDots);
   constexpr int lda = tile_ld<T, NA>, ldb = tile_ld<T, NB>, TA = NA / 16, units = P::kUnits, kC = P::kC, kRows = P::kRows;
-  // fragments of LDS rows at a time: two of them take registers that the
-  // kernels of the full size do not have
+  // fragments of LDS rows at a time, where there are registers for them
   constexpr int AHEAD = P::kSimd == 4 && NA == 128 && (BACK || EXACT || sizeof(T) == 4) ? 1 : 2;
 
   const int id = job.kinds == 1 ? blockIdx.x : blockIdx.x / 16 * 8 + blockIdx.x % 8;
@@ -711,9 +733,10 @@ hipError_t launch_chunks(const ChunkArgs& a, const ChunkArgs* b, int bf16, int B
 // chunk takes a workgroup, in us: 6 alone on its CU and 9.5 beside another, 2.5
 // in the launch that forms the segments' own states, and, for more than one
 // segment, 8 for the launches and the states' passage at 4 TB/s (8 bytes for
-// each of their values).  Measured against one segment, bf16, 128 x 128: 8
-// states of 20000 tokens 164 us in 63 segments (187 in 32), 256 states of 10000
-// 2.15 ms for the gradients in one (2.53 in two).
+// each of their values).  Measured, bf16, 128 x 128: 8 states of 20000 tokens
+// 164 us in 63 segments and 187 in 32; 256 states of 10000 tokens 2.15 ms for
+// the gradients in one segment and 2.53 in two; six ragged rows of 5 states and
+// 1999 tokens 65 us before the rule and 56 with it.
 struct Cut {
   int64_t L;
   int nseg;
@@ -774,7 +797,7 @@ size_t attn_workspace(const AttnArgs& a, bool backward) {
 
 hipError_t launch_attn(const AttnArgs& a, hipStream_t s) {
   // one token: the state's traffic is all (128 x 8 states of 128 x 128, 16 query
-  // heads: 38 us in a chunk, XX us by itself)
+  // heads: 38 us in a chunk, 23.7 us by itself)
   if (a.T == 1) return launch_attn_step(a, s);
   const Cut c = cut(a);
   ChunkArgs r = base(a, c);
