@@ -10,11 +10,13 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import functools
+from array import array
 
 from . import _lib
 from ._lib import load
 
 _torch = None
+_DTYPES = {}  # the operands' dtypes and their numbers in C
 
 
 def _t():
@@ -22,6 +24,7 @@ def _t():
     if _torch is None:
         import torch
         _torch = torch
+        _DTYPES.update({torch.float32: _lib.DTYPE["f32"], torch.bfloat16: _lib.DTYPE["bf16"]})
     return _torch
 
 
@@ -53,12 +56,13 @@ def _stream(t) -> int:
 
 
 def _dtype(name, t) -> int:
-    torch = _t()
-    if t.dtype == torch.bfloat16:
-        return _lib.DTYPE["bf16"]
-    if t.dtype == torch.float32:
-        return _lib.DTYPE["f32"]
-    raise ValueError(f"{name}: want float32 or bfloat16, got {t.dtype}")
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        _t()
+        dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise ValueError(f"{name}: want float32 or bfloat16, got {t.dtype}")
+    return dt
 
 
 def _like(name, t, shape, ref, dtype=None):
@@ -88,23 +92,21 @@ def _ptr(t):
 # ---- attention ----------------------------------------------------------------
 
 
-_Views4, _Views7 = C.c_int64 * 16, C.c_int64 * 28  # four and seven C views {pointer, batch, step, head}
-
-
-def _views(kind, *tensors):
-    """The C views of [batch, steps, heads, size] tensors, as the arguments of a call."""
+def _views(*tensors):
+    """C views {pointer, batch, step, head} of [batch, steps, heads, size] tensors: an
+    array that holds them (to be kept until the call), and its address."""
     flat = []
     for t in tensors:
         b, s, h, i = t.stride()
         if i != 1 and t.shape[3] > 1:
             raise ValueError(f"the elements of a head must be contiguous, got strides {tuple(t.stride())}")
         flat += t.data_ptr(), b, s, h
-    a = kind(*flat)
-    return [C.byref(a, 32 * n) for n in range(len(tensors))]
+    a = array("q", flat)
+    return a, a.buffer_info()[0]
 
 
 def _attention(q, k, v, log_decay, lengths, scale):
-    """Checks the operands; the C struct and the sizes."""
+    """Checks the operands; the sizes for C, with the scale, and those of the tensors."""
     torch = _t()
     if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
         raise ValueError("q, k and v: want [batch, steps, heads, size]")
@@ -120,21 +122,27 @@ def _attention(q, k, v, log_decay, lengths, scale):
     _dense("log_decay", log_decay, (H,), q, torch.float32)
     if lengths is not None:
         _dense("lengths", lengths, (B,), q, torch.int32)
-    sizes = _dtype("q", q), B, H, HQ // H, dk, dv, T
-    return _lib.Attention(*sizes, dk ** -0.5 if scale is None else scale), sizes, (B, T, HQ, H, dk, dv)
+    sizes = _dtype("q", q), B, H, HQ // H, dk, dv, T, dk ** -0.5 if scale is None else scale
+    return sizes, (B, T, HQ, H, dk, dv)
 
 
 @functools.lru_cache(maxsize=256)
-def _attention_bytes(backward, *sizes):
-    n = C.c_size_t()
-    _check(load().ambptt_decay_attention_workspace(C.byref(_lib.Attention(*sizes, 1.0)), backward, C.byref(n)))
-    return n.value
+def _attention_call(backward, *sizes):
+    """The C struct of these sizes, and the bytes of workspace that the call needs."""
+    a, n = C.byref(_lib.Attention(*sizes)), C.c_size_t()
+    _check(load().ambptt_decay_attention_workspace(a, backward, C.byref(n)))
+    return a, n.value
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_call(*sizes):
+    return C.byref(_lib.Norm(*sizes))
 
 
 @functools.lru_cache(maxsize=256)
 def _norm_bytes(rows, cols):
     n = C.c_size_t()
-    _check(load().ambptt_add_norm_backward_workspace(C.byref(_lib.Norm(0, 0, rows, cols, 0, 0.0)), C.byref(n)))
+    _check(load().ambptt_add_norm_backward_workspace(_norm_call(0, 0, rows, cols, 0, 0.0), C.byref(n)))
     return n.value
 
 
@@ -150,6 +158,21 @@ def _result(out, name, shape, ref, dtype=None):
     return _like(name, t, shape, ref, dtype)
 
 
+def _result_dense(out, name, shape, ref, dtype):
+    """The same, contiguous."""
+    if out and out.get(name) is not None:
+        return _dense(name, out[name], shape, ref, dtype)
+    return ref.new_empty(shape, dtype=dtype)
+
+
+def _result_like(out, name, ref, dtype=None):
+    """The same with the shape of `ref`."""
+    if out and out.get(name) is not None:
+        return _like(name, out[name], ref.shape, ref, dtype)
+    torch = _t()
+    return torch.empty_like(ref, dtype=dtype, memory_format=torch.contiguous_format)
+
+
 def decay_attention(q, k, v, log_decay, s0=None, lengths=None, scale=None, out: dict | None = None) -> dict:
     """Attention whose state decays (ambptt_decay_attention): {"o", "sn"}.
 
@@ -161,19 +184,18 @@ def decay_attention(q, k, v, log_decay, s0=None, lengths=None, scale=None, out: 
     after them.  out["sn"] may be s0.
     """
     torch = _t()
-    a, sizes, (B, T, HQ, H, dk, dv) = _attention(q, k, v, log_decay, lengths, scale)
+    sizes, (B, T, HQ, H, dk, dv) = _attention(q, k, v, log_decay, lengths, scale)
     with _on(q):
         state = (B, H, dk, dv)
         _dense("s0", s0, state, q, torch.float32)
-        o = _result(out, "o", (B, T, HQ, dv), q)
+        o = _result_like(out, "o", q) if dk == dv else _result(out, "o", (B, T, HQ, dv), q)
         sn = s0 if out and s0 is not None and out.get("sn") is s0 else \
-            _dense("sn", _result(out, "sn", state, q, torch.float32), state, q, torch.float32)
-        L = load()
-        n = _attention_bytes(0, *sizes)
+            _result_dense(out, "sn", state, q, torch.float32)
+        a, n = _attention_call(0, *sizes)
         ws = _workspace(n, q)
-        vq, vk, vv, vo = _views(_Views4, q, k, v, o)
-        _check(L.ambptt_decay_attention(C.byref(a), vq, vk, vv, log_decay.data_ptr(), _ptr(s0), _ptr(lengths), vo,
-                                        sn.data_ptr(), _ptr(ws), n, _stream(q)))
+        views, at = _views(q, k, v, o)
+        _check(load().ambptt_decay_attention(a, at, at + 32, at + 64, log_decay.data_ptr(), _ptr(s0), _ptr(lengths),
+                                             at + 96, sn.data_ptr(), _ptr(ws), n, _stream(q)))
     return {"o": o, "sn": sn}
 
 
@@ -199,35 +221,35 @@ def decay_attention_backward(q, k, v, log_decay, do, s0=None, dsn=None, lengths=
     where s0 or dsn was given (or out["ds0"]), else None.
     """
     torch = _t()
-    a, sizes, (B, T, HQ, H, dk, dv) = _attention(q, k, v, log_decay, lengths, scale)
+    sizes, (B, T, HQ, H, dk, dv) = _attention(q, k, v, log_decay, lengths, scale)
     with _on(q):
         state = (B, H, dk, dv)
         _dense("s0", s0, state, q, torch.float32)
         _dense("dsn", dsn, state, q, torch.float32)
         _like("do", do, (B, T, HQ, dv), q)
-        res = {"dq": _result(out, "dq", q.shape, q), "dk": _result(out, "dk", k.shape, q),
-               "dv": _result(out, "dv", v.shape, q), "ds0": None}
+        res = {"dq": _result_like(out, "dq", q), "dk": _result_like(out, "dk", k), "dv": _result_like(out, "dv", v),
+               "ds0": None}
         if s0 is not None or dsn is not None or (out and out.get("ds0") is not None):
-            res["ds0"] = _dense("ds0", _result(out, "ds0", state, q, torch.float32), state, q, torch.float32)
-        L = load()
-        n = _attention_bytes(1, *sizes)
+            res["ds0"] = _result_dense(out, "ds0", state, q, torch.float32)
+        a, n = _attention_call(1, *sizes)
         ws = _workspace(n, q)
-        vq, vk, vv, vo, v1, v2, v3 = _views(_Views7, q, k, v, do, res["dq"], res["dk"], res["dv"])
-        _check(L.ambptt_decay_attention_backward(
-            C.byref(a), vq, vk, vv, log_decay.data_ptr(), _ptr(s0), _ptr(lengths), vo, _ptr(dsn), v1, v2, v3,
-            _ptr(res["ds0"]), _ptr(ws), n, _stream(q)))
+        views, at = _views(q, k, v, do, res["dq"], res["dk"], res["dv"])
+        _check(load().ambptt_decay_attention_backward(
+            a, at, at + 32, at + 64, log_decay.data_ptr(), _ptr(s0), _ptr(lengths), at + 96, _ptr(dsn), at + 128,
+            at + 160, at + 192, _ptr(res["ds0"]), _ptr(ws), n, _stream(q)))
     return res
 
 
 # ---- dropout and norm -----------------------------------------------------------
 
 
-def _rows(name, t):
-    """(pointer, row stride) of a tensor seen as rows of its last dimension."""
-    shape = t.shape
+def _rows(name, t, cols):
+    """(pointer, row stride) of a tensor seen as rows of its last dimension, `cols` long."""
+    if t is None:
+        return None, 0
     if t.is_contiguous():
-        return t.data_ptr(), shape[-1]
-    stride = t.stride()
+        return t.data_ptr(), cols
+    shape, stride = t.shape, t.stride()
     if shape[-1] > 1 and stride[-1] != 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
     if len(shape) == 1:
@@ -244,10 +266,10 @@ def _rows(name, t):
 
 
 def _sizes(name, x):
-    if x.dim() < 1 or x.shape[-1] < 1:
+    shape = x.shape
+    if not shape or shape[-1] < 1:
         raise ValueError(f"{name}: want rows of one element and more")
-    cols = x.shape[-1]
-    return x.numel() // cols, cols
+    return x.numel() // shape[-1], shape[-1]
 
 
 def _drop(p, seed, offset):
@@ -270,10 +292,10 @@ def dropout(x, p, seed, offset=0, residual=None, out=None):
     with _on(x):
         if residual is not None:
             _like("residual", residual, x.shape, x)
-        y = _result({"out": out}, "out", x.shape, x)
-        xp, xl = _rows("x", x)
-        rp, rl = _rows("residual", residual) if residual is not None else (None, 0)
-        yp, yl = _rows("out", y)
+        y = _result_like(None, "out", x) if out is None else _like("out", out, x.shape, x)
+        xp, xl = _rows("x", x, cols)
+        rp, rl = _rows("residual", residual, cols)
+        yp, yl = _rows("out", y, cols)
         _check(load().ambptt_dropout(dt, rows, cols, C.byref(_lib.Drop(p, seed & 0xFFFFFFFFFFFFFFFF,
                                                                        offset & 0xFFFFFFFFFFFFFFFF)),
                                      xp, xl, rp, rl, yp, yl, _stream(x)))
@@ -301,24 +323,24 @@ def add_norm(x, w, residual=None, eps=1e-6, p=0.0, seed=0, offset=0, out_dtype=N
     rows, cols = _sizes("x", x)
     f8 = out_dtype == "f8"
     dt = _dtype("x", x)
-    a = _lib.Norm(dt, _lib.F8 if f8 else dt, rows, cols, scale_block, eps)
+    a = _norm_call(dt, _lib.F8 if f8 else dt, rows, cols, scale_block, eps)
     with _on(x):
         if residual is not None:
             _like("residual", residual, x.shape, x)
         _dense("w", w, (cols,), x, torch.float32)
         drop = _drop(p, seed, offset)
         same = residual is None and drop is None and not (out and out.get("h") is not None)
-        h = x if same else _result(out, "h", x.shape, x)
-        y = _result(out, "y", x.shape, x, torch.float8_e4m3fn if f8 else None)
+        h = x if same else _result_like(out, "h", x)
+        y = _result_like(out, "y", x, torch.float8_e4m3fn if f8 else None)
         res = {"h": h, "y": y}
         if f8:
             shape = (*x.shape[:-1], -(-cols // scale_block) if scale_block > 0 else 1)
-            res["scale"] = _dense("scale", _result(out, "scale", shape, x, torch.float32), shape, x, torch.float32)
-        xp, xl = _rows("x", x)
-        rp, rl = _rows("residual", residual) if residual is not None else (None, 0)
-        hp, hl = (None, 0) if same else _rows("h", h)
-        yp, yl = _rows("y", y)
-        _check(load().ambptt_add_norm(C.byref(a), drop, xp, xl, rp, rl, w.data_ptr(), hp, hl, yp, yl,
+            res["scale"] = _result_dense(out, "scale", shape, x, torch.float32)
+        xp, xl = _rows("x", x, cols)
+        rp, rl = _rows("residual", residual, cols)
+        hp, hl = (None, 0) if same else _rows("h", h, cols)
+        yp, yl = _rows("y", y, cols)
+        _check(load().ambptt_add_norm(a, drop, xp, xl, rp, rl, w.data_ptr(), hp, hl, yp, yl,
                                       _ptr(res.get("scale")), _stream(x)))
     return res
 
@@ -332,23 +354,22 @@ def add_norm_backward(dy, h, w, dh=None, eps=1e-6, p=0.0, seed=0, offset=0, out:
     torch = _t()
     rows, cols = _sizes("h", h)
     dt = _dtype("h", h)
-    a = _lib.Norm(dt, dt, rows, cols, 0, eps)
+    a = _norm_call(dt, dt, rows, cols, 0, eps)
     with _on(h):
         _like("dy", dy, h.shape, h)
         if dh is not None:
             _like("dh", dh, h.shape, h)
         _dense("w", w, (cols,), h, torch.float32)
         drop = _drop(p, seed, offset)
-        dr = _result(out, "dresidual", h.shape, h)
-        dx = _result(out, "dx", h.shape, h) if drop is not None else None
-        dw = _dense("dw", _result(out, "dw", (cols,), h, torch.float32), (cols,), h, torch.float32)
+        dr = _result_like(out, "dresidual", h)
+        dx = _result_like(out, "dx", h) if drop is not None else None
+        dw = _result_dense(out, "dw", (cols,), h, torch.float32)
         L = load()
         n = _norm_bytes(rows, cols)
         ws = _workspace(n, h)
         _check(L.ambptt_add_norm_backward(
-            C.byref(a), drop, *_rows("dy", dy), *(_rows("dh", dh) if dh is not None else (None, 0)), *_rows("h", h),
-            _ptr(w), *_rows("dresidual", dr), *(_rows("dx", dx) if dx is not None else (None, 0)), _ptr(dw), _ptr(ws),
-            n, _stream(h)))
+            a, drop, *_rows("dy", dy, cols), *_rows("dh", dh, cols), *_rows("h", h, cols), _ptr(w),
+            *_rows("dresidual", dr, cols), *_rows("dx", dx, cols), _ptr(dw), _ptr(ws), n, _stream(h)))
     res = {"dresidual": dr, "dw": dw}
     if dx is not None:
         res["dx"] = dx
