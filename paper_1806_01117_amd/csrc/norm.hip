@@ -155,19 +155,23 @@ __global__ __launch_bounds__(kThreads) void dropout(DropoutArgs a, Pieces w) {
 }
 
 // The norm's rows.  A row of up to THREADS * NV * 8 columns is read once and
-// stays in the registers of one wave (THREADS 64, four rows to a workgroup) or
-// of a workgroup, NV pieces of eight columns to a lane; longer rows (NV 0) are
-// read again for each pass over them by one workgroup.
+// stays in the registers of one wave or of a part of it (THREADS up to 64, 256
+// lanes to a workgroup) or of a workgroup, NV pieces of eight columns to a lane;
+// longer rows (NV 0) are read again for each pass over them by one workgroup.
 template <int THREADS>
-constexpr int kRowsPer = THREADS == 64 ? 4 : 1;
+constexpr int kRowsPer = THREADS <= 64 ? 256 / THREADS : 1;
 template <int THREADS>
 constexpr int kBlock = THREADS * kRowsPer<THREADS>;
+template <int THREADS>
+constexpr int kWaves = THREADS < 64 ? 1 : THREADS / 64;  // of a row
+template <int THREADS>
+constexpr int kLanes = THREADS < 64 ? THREADS : 64;  // of a row in a wave
 
 // the sum (or the maximum) over a row's threads, in each of them; a fixed order
 template <int THREADS, bool MAX>
 __device__ __forceinline__ float row_all(float v, float* lds) {
 #pragma unroll
-  for (int o = 32; o; o >>= 1) {
+  for (int o = kLanes<THREADS> / 2; o; o >>= 1) {
     const float u = __shfl_xor(v, o);
     v = MAX ? fmaxf(v, u) : v + u;
   }
@@ -185,7 +189,7 @@ __device__ __forceinline__ float row_all(float v, float* lds) {
 template <int THREADS>
 __device__ __forceinline__ void row_sums(float& v, float& u, float* lds) {
 #pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o), u += __shfl_xor(u, o);
+  for (int o = kLanes<THREADS> / 2; o; o >>= 1) v += __shfl_xor(v, o), u += __shfl_xor(u, o);
   if constexpr (THREADS > 64) {
     __syncthreads();
     if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v, lds[THREADS / 64 + threadIdx.x / 64] = u;
@@ -234,8 +238,8 @@ __device__ __forceinline__ float most_of(const float (&y)[kV]) {
 }
 
 // stores h and y of columns c .. c + 7; every lane of the row comes here (16 of
-// them share a block's maximum); `most` is the row's
-template <class T, bool F8>
+// them, or all of a shorter row, share a block's maximum); `most` is the row's
+template <class T, int THREADS, bool F8>
 __device__ __forceinline__ void store_y(const float (&h)[kV], float (&y)[kV], float most, const NormArgs& a, int64_t r, int c) {
   if (a.h.p && c < a.cols) store8(h, row_of<T>(a.h, r), c, a.cols);
   if constexpr (!F8) {
@@ -244,7 +248,7 @@ __device__ __forceinline__ void store_y(const float (&h)[kV], float (&y)[kV], fl
     if (a.block) {
       most = most_of(y);
 #pragma unroll
-      for (int o = 8; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+      for (int o = THREADS < 16 ? THREADS / 2 : 8; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
     }
     if (c >= a.cols) return;
     // a normal number: one that lost bits would take what it divides out of range
@@ -266,7 +270,7 @@ __device__ __forceinline__ void store_y(const float (&h)[kV], float (&y)[kV], fl
 
 template <class T, int THREADS, int NV, bool F8>
 __global__ __launch_bounds__(kBlock<THREADS>) void add_norm(NormArgs a) {
-  __shared__ float lds[THREADS / 64 + 1];
+  __shared__ float lds[kWaves<THREADS>];
   const int64_t wide = (a.cols + kV - 1) / kV, rows = kRowsPer<THREADS>;
   const int lane = threadIdx.x % THREADS;
   const float inv = 1.0f / float(a.cols);
@@ -288,7 +292,7 @@ __global__ __launch_bounds__(kBlock<THREADS>) void add_norm(NormArgs a) {
       }
       if (F8 && !a.block) most = row_all<THREADS, true>(most, lds);
 #pragma unroll
-      for (int k = 0; k < NV; ++k) store_y<T, F8>(h[k], y[k], most, a, r, (k * THREADS + lane) * kV);
+      for (int k = 0; k < NV; ++k) store_y<T, THREADS, F8>(h[k], y[k], most, a, r, (k * THREADS + lane) * kV);
     } else {
       float sum = 0.0f, most = 0.0f, h[kV], y[kV];
       for (int c = lane * kV; c < a.cols; c += THREADS * kV) {
@@ -309,7 +313,7 @@ __global__ __launch_bounds__(kBlock<THREADS>) void add_norm(NormArgs a) {
         const int c = c0 + lane * kV;
         load_h<T>(h, a, r, c, wide);
         times_w(y, h, rr, a, c);
-        store_y<T, F8>(h, y, most, a, r, c);  // h may be x or the residual: this piece is not read again
+        store_y<T, THREADS, F8>(h, y, most, a, r, c);  // h may be x or the residual: this piece is not read again
       }
     }
   }
@@ -333,8 +337,8 @@ __device__ __forceinline__ void zero8(float (&v)[kV]) {
 // Four waves to a SIMD: what norm_grad_parts counts on.
 template <class T, int THREADS, int NV>
 __global__ __launch_bounds__(kBlock<THREADS>, 4) void add_norm_backward(NormGradArgs a) {
-  __shared__ float lds[2 * (THREADS / 64)];
-  extern __shared__ float sums[];  // THREADS 64: the waves' sums
+  __shared__ float lds[2 * kWaves<THREADS>];
+  extern __shared__ float sums[];  // THREADS up to 64: the sums of the workgroup's rows
   const int64_t wide = (a.cols + kV - 1) / kV, rows = kRowsPer<THREADS>;
   const int lane = threadIdx.x % THREADS, row = threadIdx.x / THREADS;
   const float inv = 1.0f / float(a.cols);
@@ -376,7 +380,7 @@ __global__ __launch_bounds__(kBlock<THREADS>, 4) void add_norm_backward(NormGrad
       }
     }
     if (!a.dw) return;
-    if constexpr (THREADS == 64) {
+    if constexpr (THREADS <= 64) {
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * THREADS + lane) * kV;
@@ -429,27 +433,34 @@ __global__ __launch_bounds__(kBlock<THREADS>, 4) void add_norm_backward(NormGrad
   }
 }
 
-// dw = the sum of `parts` rows: 32 columns to a workgroup, every eighth row to a
-// thread, then those eight, in a fixed order
-__global__ __launch_bounds__(kThreads) void sum_parts(const float* p, int parts, int cols, float* out) {
-  __shared__ float lds[8][32];
-  const int c = blockIdx.x * 32 + threadIdx.x % 32, k = threadIdx.x / 32;
-  float v = 0.0f;
-  if (c < cols) {
+// dw = the sum of `parts` rows: 32 columns to a workgroup and turn, every 32nd
+// row to a thread, then those 32, in a fixed order
+__global__ __launch_bounds__(1024) void sum_parts(const float* p, int parts, int cols, float* out) {
+  __shared__ float lds[32][33];
+  const int n = threadIdx.x % 32, k = threadIdx.x / 32;
+  for (int64_t c = int64_t(blockIdx.x) * 32; c < cols; c += int64_t(gridDim.x) * 32) {
+    float v = 0.0f;
+    if (c + n < cols) {
 #pragma unroll 8
-    for (int i = k; i < parts; i += 8) v += p[int64_t(i) * cols + c];
-  }
-  lds[k][threadIdx.x % 32] = v;
-  __syncthreads();
-  if (k || c >= cols) return;
+      for (int i = k; i < parts; i += 32) v += p[int64_t(i) * cols + c + n];
+    }
+    lds[n][k] = v;
+    __syncthreads();
+    v = lds[k][n];  // a column in 32 neighbouring lanes
 #pragma unroll
-  for (int i = 1; i < 8; ++i) v += lds[i][threadIdx.x];
-  out[c] = v;
+    for (int o = 16; o; o >>= 1) v += __shfl_xor(v, o);
+    if (n == 0 && c + k < cols) out[c + k] = v;
+    __syncthreads();
+  }
 }
 
-// Threads to a row and pieces to a lane: one wave while that takes two pieces,
-// then workgroups with one piece to a lane, up to the largest.  Measured, us
-// forward and backward with 20000 rows of bf16:
+// Threads to a row and pieces to a lane: a part of a wave that the row fills, one
+// wave while that takes two pieces, then workgroups with one piece to a lane, up
+// to the largest.  Measured, us forward and backward, with 100000 rows of bf16:
+//   64 columns   8 x 1   10.1 14.5    16 x 1 13.0 14.8    64 x 1 37.7 34.8
+//   128          16 x 1  17.8 17.8    32 x 1 24.1 22.5    64 x 1 38.4 36.7
+//   256          32 x 1  31.4 29.6    64 x 1 42.8 38.7
+// and with 20000:
 //   512 columns  64 x 1  13.9 20.4    256 x 1 25.6 36.6
 //   1024         64 x 2  28.4 30.1    256 x 1 30.7 38.1
 //   2048         256 x 1 57.9 49.1    64 x 4  64.9 54.0
@@ -460,6 +471,9 @@ struct Form {
   int threads, nv;
 };
 Form form_of(int64_t cols) {
+  if (cols <= 64) return {8, 1};
+  if (cols <= 128) return {16, 1};
+  if (cols <= 256) return {32, 1};
   if (cols <= 512) return {64, 1};
   if (cols <= 1024) return {64, 2};
   if (cols <= 2048) return {256, 1};
@@ -480,7 +494,7 @@ hipError_t run_norm(const NormArgs& a, hipStream_t s) {
 }
 template <class T, int THREADS, int NV>
 hipError_t run_norm_backward(const NormGradArgs& a, hipStream_t s) {
-  const unsigned grid = unsigned(norm_grad_parts(a.rows, a.cols)), lds = THREADS == 64 ? 4 * a.cols * 4 : 0;
+  const unsigned grid = unsigned(norm_grad_parts(a.rows, a.cols)), lds = THREADS <= 64 ? kRowsPer<THREADS> * a.cols * 4 : 0;
   add_norm_backward<T, THREADS, NV><<<grid, kBlock<THREADS>, lds, s>>>(a);
   return hipGetLastError();
 }
@@ -488,6 +502,9 @@ hipError_t run_norm_backward(const NormGradArgs& a, hipStream_t s) {
 #define BY_FORM(run, T, a, s)                        \
   const Form f = form_of(a.cols);                    \
   switch (f.threads + f.nv) {                        \
+    case 8 + 1: return run<T, 8, 1>(a, s);           \
+    case 16 + 1: return run<T, 16, 1>(a, s);         \
+    case 32 + 1: return run<T, 32, 1>(a, s);         \
     case 64 + 1: return run<T, 64, 1>(a, s);         \
     case 64 + 2: return run<T, 64, 2>(a, s);         \
     case 256 + 1: return run<T, 256, 1>(a, s);       \
@@ -544,7 +561,7 @@ hipError_t launch_add_norm(const NormArgs& a, hipStream_t s) {
 // more than there are rows for
 int norm_grad_parts(int64_t rows, int64_t cols) {
   const int threads = form_of(cols).threads;
-  const int64_t groups = threads == 64 ? (rows + 3) / 4 : rows, most = threads == 64 ? 1024 : 262144 / threads;
+  const int64_t per = threads <= 64 ? 256 / threads : 1, groups = (rows + per - 1) / per, most = 262144 / (threads * per);
   return int(groups < 1 ? 1 : groups < most ? groups : most);
 }
 
@@ -554,7 +571,8 @@ hipError_t launch_add_norm_backward(const NormGradArgs& a, hipStream_t s) {
     if (e != hipSuccess) return e;
   }
   if (!a.dw) return hipSuccess;
-  sum_parts<<<unsigned((a.cols + 31) / 32), kThreads, 0, s>>>(a.parts, a.rows ? norm_grad_parts(a.rows, a.cols) : 0, a.cols, a.dw);
+  const int64_t sums = (int64_t(a.cols) + 31) / 32;
+  sum_parts<<<unsigned(sums < 65536 ? sums : 65536), 1024, 0, s>>>(a.parts, a.rows ? norm_grad_parts(a.rows, a.cols) : 0, a.cols, a.dw);
   return hipGetLastError();
 }
 

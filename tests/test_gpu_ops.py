@@ -513,6 +513,16 @@ def test_norm_in_8_bits(amb, dtype, rows, cols, block):
     assert (d <= 1.001 * np.abs(y) * 2.0 ** -4 + s * 2.0 ** -10).all() and np.abs(_np(got["y"].float())).max() <= 448
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(2, 16), (100, 20), (37, 33), (2000, 61), (70, 65), (41, 128), (33, 200), (40000, 24), (19, 256),
+                                       (9, 257), (1500, 512)])
+def test_norm_of_narrow_rows(amb, dtype, rows, cols):
+    # a part of a wave to a row: full and partial waves and workgroups, with and without 8 bits
+    test_norm(amb, dtype, rows, cols, 0.25)
+    for block in (0, 128):
+        test_norm_in_8_bits(amb, dtype, rows, cols, block)
+
+
 @pytest.mark.parametrize("block", [0, 128])
 def test_norm_in_8_bits_below_the_normal_numbers(amb, block):
     # a scale that lost its bits would take the stored values past 448: it is 2^-126 at least
