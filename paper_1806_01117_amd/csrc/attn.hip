@@ -357,6 +357,12 @@ struct Plan {
   static constexpr int kTileA = kC * tile_ld<T, NA>, kTileB = kC * tile_ld<T, NB>;
   static constexpr int kDots = kRows * kUnits * Mm<T>::kHalves * 1024;    // the exchanged products
   static constexpr int kLds = 2 * kTileA + kTileB + kDots + int(sizeof(Tables));
+  // The loops over the state's rows end at the last that is there.  Only in fp32
+  // with 128 of them: 8 rows of 2000 tokens, 16 states, take 395 us so and 491
+  // without (128 x 128; the loops' bodies then take fewer registers too), 2 of
+  // 3000 tokens, 4 states of 96 x 96, 48 and 59.  With 64 it cost 3 %, and in
+  // bf16, whose loops are shorter, 15 %.
+  static constexpr bool kBreaks = sizeof(T) == 4 && NA == 128;
   // waves of a SIMD: four, and as many workgroups as LDS holds where they have one to each
   static constexpr int kSimd = kWaves > 4 || 163840 / kLds > 4 ? 4 : 163840 / kLds;
 };
@@ -366,8 +372,9 @@ struct Plan {
 // parts are in registers (AHEAD: fragments of u on their way)
 template <class T, int NA, int PARTS, int AHEAD, int GO>
 __device__ __forceinline__ void update(f4 (&S)[NA / 16], float whole, typename Mm<T>::Frag (&w)[kTileRows<T> / Mm<T>::kTiles],
-                                       unsigned state_at, const float* weight) {
+                                       unsigned state_at, const float* weight, int na) {
   typedef Mm<T> M;
+  typedef Plan<T, NA, NA> P;
   constexpr int units = kTileRows<T> / M::kTiles, ld = tile_ld<T, NA>;
 #pragma unroll
   for (int u = 0; u < units; u += GO) {
@@ -387,11 +394,12 @@ __device__ __forceinline__ void update(f4 (&S)[NA / 16], float whole, typename M
     auto columns = [&](int d) {
       const unsigned at = M::state_tile(state_at, d);
 #pragma unroll
-      for (int i = 0; i < GO; ++i) f[d % AHEAD][i] = M::token(at + Plan<T, NA, NA>::kTileA, ld, u + i);
+      for (int i = 0; i < GO; ++i) f[d % AHEAD][i] = M::token(at + P::kTileA, ld, u + i);
     };
     if (AHEAD > 1) columns(0);
 #pragma unroll
     for (int d = 0; d < NA / 16; ++d) {
+      if (P::kBreaks && 16 * d >= na) break;
       if (AHEAD == 1 || d + 1 < NA / 16) columns(AHEAD == 1 ? d : d + 1);  // two: on their way during this tile's products
       f4 sum = {0, 0, 0, 0};
 #pragma unroll
@@ -489,6 +497,7 @@ __global__ __launch_bounds__(64 * (NB / 16), (Plan<T, NA, NB>::kSimd)) void chun
           f4 p[M::kTiles] = {};
 #pragma unroll
           for (int d0 = 0; d0 < NA * int(sizeof(T)) / 64; d0 += 2) {
+            if (P::kBreaks && 16 * d0 >= a.na) break;
             Frag cf[2], uf[M::kTiles][2];
 #pragma unroll
             for (int d = 0; d < 2; ++d) {
@@ -530,6 +539,7 @@ __global__ __launch_bounds__(64 * (NB / 16), (Plan<T, NA, NB>::kSimd)) void chun
           if (AHEAD > 1) rows(0);
 #pragma unroll
           for (int d = 0; d < TA / M::kTiles; ++d) {
+            if (P::kBreaks && 16 * d >= a.na) break;
             if (AHEAD == 1 || d + 1 < TA / M::kTiles) rows(AHEAD == 1 ? d : d + 1);  // two: on their way during this unit's products
             f4 s[M::kTiles];
 #pragma unroll
@@ -633,7 +643,7 @@ __global__ __launch_bounds__(64 * (NB / 16), (Plan<T, NA, NB>::kSimd)) void chun
         // S = lambda^m S + sum of u (weight w)^T
         const float whole = BACK && q ? 1.0f : m == kC ? full : power(ld, m);
         constexpr int go = P::kSimd == 4 && NA == 128 && OUT && EXACT ? 1 : units;
-        update<T, NA, EXACT || M::kParts == 1 ? M::kParts : 2, AHEAD, go>(S, whole, w, state_at, tab->weight);
+        update<T, NA, EXACT || M::kParts == 1 ? M::kParts : 2, AHEAD, go>(S, whole, w, state_at, tab->weight, a.na);
       }
       __syncthreads();
     }

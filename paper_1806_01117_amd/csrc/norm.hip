@@ -565,14 +565,17 @@ int norm_grad_parts(int64_t rows, int64_t cols) {
   return int(groups < 1 ? 1 : groups < most ? groups : most);
 }
 
-hipError_t launch_add_norm_backward(const NormGradArgs& a, hipStream_t s) {
+hipError_t launch_add_norm_backward(const NormGradArgs& in, hipStream_t s) {
+  NormGradArgs a = in;
+  const int parts = norm_grad_parts(a.rows, a.cols);
+  if (parts == 1) a.parts = a.dw;  // one part is the sum
   if (a.rows) {
     const hipError_t e = a.bf16 ? norm_backward_by_form<__bf16>(a, s) : norm_backward_by_form<float>(a, s);
     if (e != hipSuccess) return e;
   }
-  if (!a.dw) return hipSuccess;
+  if (!a.dw || (parts == 1 && a.rows)) return hipSuccess;
   const int64_t sums = (int64_t(a.cols) + 31) / 32;
-  sum_parts<<<unsigned(sums < 65536 ? sums : 65536), 1024, 0, s>>>(a.parts, a.rows ? norm_grad_parts(a.rows, a.cols) : 0, a.cols, a.dw);
+  sum_parts<<<unsigned(sums < 65536 ? sums : 65536), 1024, 0, s>>>(a.parts, a.rows ? parts : 0, a.cols, a.dw);
   return hipGetLastError();
 }
 
