@@ -31,7 +31,7 @@
 // instructions take 62 % of a SIMD's time and matrix instructions 39 %, that is
 // all of it; dq 821 us with one workgroup to a CU, 46 % and 27 %, the rest being
 // what its waves wait for each other at the two barriers of a chunk.  The prompt
-// takes 166 us, 2.5 TB/s, 52 % and 28 % in the launch that writes the results.
+// takes 168 us, 2.4 TB/s, 52 % and 28 % in the launch that writes the results.
 // In fp32 matrix instructions alone take 53 % (forwards) and 65 % (backwards).
 //
 // Rounding.  States, accumulators and sums are fp32, and bf16 operands enter
