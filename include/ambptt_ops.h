@@ -15,6 +15,7 @@
  *     the *_workspace call, 256-byte aligned).  Calls in flight at the same
  *     time need workspaces of their own.
  *   - Two runs on the same inputs give the same bits.
+ *   - No output overlaps an input or another output, save where a call says so.
  *   - EINVAL / EUNSUPPORTED: nothing was enqueued.  EHIP: a launch failed.
  *   - Operands are fp32 or bf16 (AMBPTT_F32, AMBPTT_BF16); states, decays,
  *     norm weights and their gradients, scales, sums and statistics are fp32.
@@ -78,8 +79,9 @@ ambptt_status ambptt_decay_attention(const ambptt_attention* a, const ambptt_vie
                                      size_t workspace_bytes, void* stream);
 
 /* Gradients of q, k, v and, where ds0 is given, of s0.  dsn: the gradient of
- * the last state, NULL = zeros.  The states are formed again from s0, k and v;
- * nothing is kept from the forward call. */
+ * the last state, NULL = zeros; ds0 may not be dsn (EINVAL), which is read until
+ * the end.  The states are formed again from s0, k and v; nothing is kept from
+ * the forward call. */
 ambptt_status ambptt_decay_attention_backward(const ambptt_attention* a, const ambptt_view* q, const ambptt_view* k,
                                               const ambptt_view* v, const float* log_decay, const float* s0,
                                               const int32_t* lengths, const ambptt_view* d_o, const float* dsn,
@@ -113,7 +115,8 @@ ambptt_status ambptt_dropout(int32_t dtype, int64_t rows, int64_t cols, const am
 /* ---- root-mean-square norm with the residual's addition -----------------------
  *
  *   h = residual + dropout(x),   y = w h / sqrt(mean(h^2) + eps)
- * row by row, h and y in fp32 until they are stored. */
+ * row by row, h and y in fp32 until they are stored, the mean too (a row whose
+ * squares overflow fp32 gives zeros). */
 enum { AMBPTT_F8 = 2 };  /* y in 8 bits: OCP e4m3, y ~= scale * stored, scale = max|y| / 448 and >= 2^-126 */
 
 typedef struct {

@@ -146,6 +146,7 @@ ambptt_status ambptt_decay_attention_backward(const ambptt_attention* a, const a
   REFUSE(misaligned(log_decay, 4) || misaligned(s0, 16) || misaligned(dsn, 16) || misaligned(ds0, 16) ||
              misaligned(lengths, 4),
          AMBPTT_EINVAL, "states must be aligned to 16 bytes, decays and lengths to 4");
+  REFUSE(ds0 && ds0 == dsn, AMBPTT_EINVAL, "ds0 may not be dsn");
   AttnGradArgs r{};
   r.a = attn_args(a);
   CHECK(check_workspace(workspace, workspace_bytes, attn_workspace(r.a, true)));

@@ -146,6 +146,17 @@ def test_attention_refuses_null(lib):
     assert lib.ambptt_decay_attention_workspace(ctypes.byref(a), 0, None) == EINVAL
 
 
+def test_attention_backward_refuses_its_own_gradient_of_the_state(lib):
+    from paper_1806_01117_amd import _lib
+    a = _lib.Attention(**GOOD)
+    n = ctypes.c_size_t()
+    assert lib.ambptt_decay_attention_workspace(ctypes.byref(a), 1, ctypes.byref(n)) == 0
+    v = ctypes.byref(_lib.View(p=4096, batch=100000, step=1000, head=128))
+    assert lib.ambptt_decay_attention_backward(ctypes.byref(a), v, v, v, 4096, None, None, v, 8192, v, v, v, 8192, 4096,
+                                               n.value, None) == EINVAL
+    assert b"dsn" in lib.ambptt_last_error()
+
+
 def _norm(lib, drop=None, **kw):
     from paper_1806_01117_amd import _lib
     d = dict(dtype=1, out=1, rows=4, cols=100, scale_block=0, eps=1e-6, x=4096, ldx=100, r=None, ldr=0, w=4096, h=4096,
